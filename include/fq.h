@@ -10,7 +10,8 @@
  *                step on the residual (Sec. 4.3);
  *   fq_gemm      the fallback block GEMM (Sec. 4.2 Eq. (1), Sec. 4.3 Alg. 1) for
  *                the three products of a linear layer (Sec. 3.2):
- *                Y = X W^T, dX = dY W, dW = dY^T X.
+ *                Y = X W^T, dX = dY W, dW = dY^T X;
+ *   fq_mx_*      the same layer with both operands in microscaled 4 bits.
  *
  * General rules
  *   - Every data pointer is caller-owned DEVICE memory (hipMalloc'ed or a
@@ -434,6 +435,102 @@ typedef enum fq_form {
  */
 fq_status fq_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contraction, int32_t compute_units, int biased,
                        int falls_back, int32_t form[2]);
+
+/*
+ * Microscaled 4-bit matrices: the same linear layer with the operands in 4 bits.  32 consecutive
+ * elements of a row share a power-of-two scale 2^s, stored as the byte s + 127 (E8M0); an element
+ * is stored as E2M1, a sign and one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6, and stands for
+ * that value times 2^s: 17/32 byte per element.  A ragged last group is the elements that exist.
+ * The products contract over different axes and the groups run along the contraction, so a matrix
+ * has two sides that are quantized apart: along its rows (FQ_MX_ROWS) and along its columns
+ * (FQ_MX_COLS: the groups are 32 consecutive elements of a column).
+ *
+ * Storage order of one side, R x C with the contraction along C (the columns' side of a matrix is
+ * the rows' side of its transpose), nkb = ceil(C/128):
+ *   codes: element (r, c) is half of the byte at ((r/16)*nkb + c/128)*1024 +
+ *     ((r%16) + 16*((c%128)/32))*16 + (c%32)/2, the low half for even c.  1 KiB is the operand of one
+ *     16 x 16 x 128 matrix instruction, lane by lane.
+ *   scales: group (r, c/32) is the byte at ((r/64)*nkb + c/128)*256 +
+ *     ((r%16) + 16*((c%128)/32))*4 + (r/16)%4: a lane's scales for 64 rows are one dword.
+ * Codes are padded to 16 rows, scales to 64, both to 128 along the contraction, with zeros.
+ */
+#define FQ_MX_GROUP 32
+typedef enum { FQ_MX_ROWS = 1, FQ_MX_COLS = 2, FQ_MX_BOTH = 3 } fq_mx_sides;
+
+/* The scale of a group with largest magnitude m, E = floor(log2 m):
+ *   FLOOR: s = max(E - 2, -127); magnitudes beyond 6 * 2^s become 6 * 2^s (the OCP microscaling
+ *     formats' rule);
+ *   COVER: the smallest s >= -127 with m <= 6 * 2^s, so that nothing is cut off.
+ * m = 0: byte 0 and codes 0. */
+typedef enum { FQ_MX_FLOOR = 0, FQ_MX_COVER = 1 } fq_mx_rule;
+
+/* A microscaled matrix.  Host struct, device pointers owned by the caller; a side that is not kept
+ * has two NULL pointers.  codes* and scales* are 16-byte aligned. */
+typedef struct {
+  int32_t rows, cols;    /* shape of the source matrix            */
+  uint8_t *codes;        /* along the rows                        */
+  uint8_t *scales;
+  uint8_t *codes_t;      /* along the columns (of the transpose)  */
+  uint8_t *scales_t;
+} fq_mx_tensor;
+
+/* Bytes of device memory fq_mx_bind needs; 0 on invalid arguments (negative sizes, unknown sides,
+ * more than 2^23 blocks of 128 x 128).  Host-only. */
+size_t fq_mx_bytes(int32_t rows, int32_t cols, int32_t sides);
+
+/* Carve the buffers of `out` from `base` (device, 256-byte aligned).  Host-only. */
+fq_status fq_mx_bind(void *base, int32_t rows, int32_t cols, int32_t sides, fq_mx_tensor *out);
+
+/*
+ * Quantize x_bf16 (device, row-major [rows, ld] bf16) to the sides that `out` keeps, in one launch
+ * and one read of x.  An element becomes the E2M1 value nearest to |x| / 2^s, ties to the even
+ * code, with its sign.  A group that holds an infinity or NaN gets scale byte 255 and codes 0: each
+ * of its elements then stands for NaN.  With FQ_MX_COVER the magnitude that a value beyond
+ * 3.5 * 2^126 rounds to is 2^128, which reads back as infinity.
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (rows/cols < 0, ld < cols, out's shape or alignment, too
+ * large), FQ_ERR_ENUM (rule), FQ_ERR_HIP.  rows == 0 or cols == 0 is valid and launches nothing.
+ */
+fq_status fq_mx_quantize(const void *x_bf16, int32_t rows, int32_t cols, int64_t ld, fq_mx_rule rule,
+                         fq_mx_tensor *out, void *hip_stream);
+
+/*
+ * The same with stochastic rounding and FQ_MX_COVER, for gradients: with t = |x| / 2^s cut to a
+ * multiple of 2^-17, lo and hi the E2M1 values around it and u 16 random bits, the code is hi if
+ * (t - lo) / (hi - lo) + u / 2^16 >= 1 and lo otherwise.  Element (r, c) takes half c % 2 (the low
+ * half first) of word (c / 2) % 4 of Philox4x32-10 with key `seed` and counter (c / 8, r, 0, 0);
+ * both sides take the same bits.  Results depend on (x, seed) only.
+ */
+fq_status fq_mx_quantize_sr(const void *x_bf16, int32_t rows, int32_t cols, int64_t ld, uint64_t seed,
+                            fq_mx_tensor *out, void *hip_stream);
+
+/*
+ * out[r, c] = what element (r, c) of one side (FQ_MX_ROWS or FQ_MX_COLS) stands for, as `odt`;
+ * both types hold it exactly.  out: device, row-major [rows, ldo].
+ * Errors: FQ_ERR_NULL (also a side that t does not keep), FQ_ERR_SHAPE, FQ_ERR_ENUM, FQ_ERR_HIP.
+ */
+fq_status fq_mx_dequantize(const fq_mx_tensor *t, int32_t side, void *out, fq_out_dtype odt, int64_t ldo,
+                           void *hip_stream);
+
+/*
+ * The three products of fq_op on microscaled operands (NT reads both tensors' rows' side, NN the
+ * rows' side of A and the columns' side of B, TN both columns' sides).  The products of codes and
+ * scales are exact and are added in binary32, in an order that depends on the shapes only; stored
+ * as binary32 or rounded once to bf16.  A group of scale byte 255 makes every output it enters NaN.
+ * C, ldc and errors as fq_gemm (FQ_ERR_NULL: also a side that the product needs and the tensor does
+ * not keep); FQ_ERR_SHAPE also for an output of more than 2^23 tiles of 64 x 64.
+ */
+fq_status fq_mx_gemm(fq_op op, const fq_mx_tensor *A, const fq_mx_tensor *B, void *C, fq_out_dtype cdt,
+                     int64_t ldc, void *hip_stream);
+
+/*
+ * Forward of a linear layer: Y = Q(X) W^T with X [rows, ld] in bf16, quantized along its rows by
+ * `rule`, and W quantized before (rows' side, [N, K], K = X's columns).  The same values, bit for
+ * bit, as fq_mx_quantize into `xq` and fq_mx_gemm.  xq: a tensor of X's shape that keeps its rows'
+ * side; overwritten, its contents are unspecified afterwards.
+ * Errors as those two calls.
+ */
+fq_status fq_mx_linear(const void *x_bf16, int32_t rows, int64_t ld, fq_mx_rule rule, const fq_mx_tensor *W,
+                       fq_mx_tensor *xq, void *Y, fq_out_dtype ydt, int64_t ldy, void *hip_stream);
 
 /* (With blocks of 64 or 32, k_block counts blocks of that size.)
  * The INT32 block product of k-block `k_block` alone (Alg. 1's INT x INT

@@ -24,6 +24,9 @@ FQ_CRIT_NONE, FQ_CRIT_ABSMAX_GT, FQ_CRIT_ALL, FQ_CRIT_L1_GT, FQ_CRIT_L1REL_GT, F
 FQ_OP_NT, FQ_OP_NN, FQ_OP_TN = 0, 1, 2
 FQ_OUT_F32, FQ_OUT_BF16 = 0, 1
 FQ_TILES_256x256, FQ_TILES_32x32, FQ_TILES_128x64, FQ_TILES_128x128 = 0, 1, 2, 3
+FQ_MX_GROUP = 32
+FQ_MX_ROWS, FQ_MX_COLS, FQ_MX_BOTH = 1, 2, 3
+FQ_MX_FLOOR, FQ_MX_COVER = 0, 1
 FQ_FORM_256x256, FQ_FORM_32x32, FQ_FORM_128x64, FQ_FORM_128x128, FQ_FORM_LOADERS_128x64, FQ_FORM_LOADERS_128x128, \
     FQ_FORM_LOADERS_128x256 = 0, 1, 2, 3, 4, 5, 6
 
@@ -37,7 +40,9 @@ EXPORTS = ["fq_qtensor_bytes", "fq_qtensor_bind", "fq_quantize", "fq_quantize_sr
            "fq_status_string", "fq_header_tag", "fq_ctx_packed_bytes", "fq_ctx_scales_bytes", "fq_ctx_quantize",
            "fq_ctx_dequantize", "fq_gemm_tile_plan", "fq_gemm_path", "fq_gemm_form",
            "fq_glu_forward", "fq_glu_backward", "fq_rmsnorm_forward",
-           "fq_rmsnorm_backward", "fq_rmsnorm_backward_static"]
+           "fq_rmsnorm_backward", "fq_rmsnorm_backward_static",
+           "fq_mx_bytes", "fq_mx_bind", "fq_mx_quantize", "fq_mx_quantize_sr", "fq_mx_dequantize", "fq_mx_gemm",
+           "fq_mx_linear"]
 
 
 class fq_qtensor(C.Structure):
@@ -49,6 +54,12 @@ class fq_qtensor(C.Structure):
                 ("fb_list", C.c_void_p),
                 ("fb_slot", C.c_void_p), ("res_codes", C.c_void_p), ("res_codes_t", C.c_void_p),
                 ("res_scales", C.c_void_p)]
+
+
+class fq_mx_tensor(C.Structure):
+    """Mirror of the C struct fq_mx_tensor."""
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p),
+                ("codes_t", C.c_void_p), ("scales_t", C.c_void_p)]
 
 
 class FqError(RuntimeError):
@@ -137,6 +148,22 @@ def lib():
         L.fq_gemm_path.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int, C.POINTER(C.c_int32)]
         L.fq_gemm_form.restype = C.c_int
         L.fq_gemm_form.argtypes = [C.c_int32] * 4 + [C.c_int, C.c_int, C.POINTER(C.c_int32)]
+        mx = C.POINTER(fq_mx_tensor)
+        L.fq_mx_bytes.restype = C.c_size_t
+        L.fq_mx_bytes.argtypes = [C.c_int32] * 3
+        L.fq_mx_bind.restype = C.c_int
+        L.fq_mx_bind.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, mx]
+        L.fq_mx_quantize.restype = C.c_int
+        L.fq_mx_quantize.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.c_int, mx, C.c_void_p]
+        L.fq_mx_quantize_sr.restype = C.c_int
+        L.fq_mx_quantize_sr.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.c_uint64, mx, C.c_void_p]
+        L.fq_mx_dequantize.restype = C.c_int
+        L.fq_mx_dequantize.argtypes = [mx, C.c_int32, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]
+        L.fq_mx_gemm.restype = C.c_int
+        L.fq_mx_gemm.argtypes = [C.c_int, mx, mx, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]
+        L.fq_mx_linear.restype = C.c_int
+        L.fq_mx_linear.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int, mx, mx, C.c_void_p, C.c_int, C.c_int64,
+                                   C.c_void_p]
         _lib = L
     return _lib
 
@@ -564,3 +591,94 @@ def fq_rmsnorm_backward(dy, ctx, rstd, w, n_parts=256, stream=None):
                                      parts.data_ptr(), int(n_parts), _stream_ptr(stream)),
            "fq_rmsnorm_backward")
     return dx, dw
+
+
+class MxTensor:
+    """Device buffers of one microscaled 4-bit matrix: a torch byte tensor carved up by fq_mx_bind, plus views of its
+    pieces for inspection (the storage order is in fq.h)."""
+
+    def __init__(self, rows, cols, sides=FQ_MX_ROWS, device="cuda"):
+        self.rows, self.cols, self.sides = int(rows), int(cols), int(sides)
+        nbytes = fq_mx_bytes(self.rows, self.cols, self.sides)
+        if nbytes == 0:
+            raise FqError(FQ_ERR_SHAPE, "fq_mx_bytes")
+        self.storage = _t().empty(nbytes + 256, dtype=_t().uint8, device=device)
+        base = (self.storage.data_ptr() + 255) & ~255
+        self.c = fq_mx_tensor()
+        self._ref = C.byref(self.c)
+        _check(lib().fq_mx_bind(C.c_void_p(base), self.rows, self.cols, self.sides, self._ref), "fq_mx_bind")
+
+    def view(self, field):
+        """uint8 view of one buffer, [strips, blocks, 1024] (codes) or [ceil(rows / 64), blocks, 256] (scales); None if
+        that side is not kept."""
+        ptr = getattr(self.c, field)
+        if not ptr:
+            return None
+        r, c = (self.cols, self.rows) if field.endswith("_t") else (self.rows, self.cols)
+        unit, size = (16, 1024) if field.startswith("codes") else (64, 256)
+        shape = (-(-r // unit), -(-c // 128), size)
+        off = ptr - self.storage.data_ptr()
+        return self.storage[off:off + shape[0] * shape[1] * size].view(shape)
+
+
+def fq_mx_bytes(rows, cols, sides=FQ_MX_ROWS) -> int:
+    return int(lib().fq_mx_bytes(rows, cols, sides))
+
+
+def fq_mx_quantize(x, out: MxTensor = None, sides=FQ_MX_ROWS, rule=FQ_MX_FLOOR, stream=None) -> MxTensor:
+    """x (as for fq_quantize) in microscaled 4 bits, along its rows, its columns or both; into `out` if given, whose
+    sides then count."""
+    rows, cols, ld = _bf16_matrix(x)
+    if out is None:
+        out = MxTensor(rows, cols, sides, x.device)
+    _check((_lib or lib()).fq_mx_quantize(x.data_ptr(), rows, cols, ld, int(rule), out._ref, _stream_ptr(stream)),
+           "fq_mx_quantize")
+    return out
+
+
+def fq_mx_quantize_sr(x, seed, out: MxTensor = None, sides=FQ_MX_ROWS, stream=None) -> MxTensor:
+    """As fq_mx_quantize with stochastic rounding and scales that cover every value."""
+    rows, cols, ld = _bf16_matrix(x)
+    if out is None:
+        out = MxTensor(rows, cols, sides, x.device)
+    _check((_lib or lib()).fq_mx_quantize_sr(x.data_ptr(), rows, cols, ld, C.c_uint64(seed), out._ref,
+                                             _stream_ptr(stream)), "fq_mx_quantize_sr")
+    return out
+
+
+def _output(out, shape, out_dtype, device):
+    """(the output, its FQ_OUT_*, its pitch): `out` checked, or a new tensor of `out_dtype`."""
+    torch = _t()
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=device)
+    assert out.is_cuda and out.shape == shape
+    return out, {torch.float32: FQ_OUT_F32, torch.bfloat16: FQ_OUT_BF16}[out.dtype], _pitch(out)
+
+
+def fq_mx_dequantize(t: MxTensor, side=FQ_MX_ROWS, out=None, out_dtype=None, stream=None):
+    """What the elements of one side stand for: a [rows, cols] bfloat16 (or float32) CUDA tensor."""
+    out, odt, ldo = _output(out, (t.rows, t.cols), out_dtype or _t().bfloat16, t.storage.device)
+    _check((_lib or lib()).fq_mx_dequantize(t._ref, int(side), out.data_ptr(), odt, ldo, _stream_ptr(stream)),
+           "fq_mx_dequantize")
+    return out
+
+
+def fq_mx_gemm(op, A: MxTensor, B: MxTensor, out=None, out_dtype=None, stream=None):
+    """C = A (op) B of microscaled operands; out is a 2-D float32 or bfloat16 CUDA tensor."""
+    out, cdt, ldc = _output(out, gemm_out_shape(op, A, B), out_dtype or _t().float32, A.storage.device)
+    _check((_lib or lib()).fq_mx_gemm(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, _stream_ptr(stream)),
+           "fq_mx_gemm")
+    return out
+
+
+def fq_mx_linear(x, W: MxTensor, xq: MxTensor = None, rule=FQ_MX_FLOOR, out=None, out_dtype=None, stream=None):
+    """Y = Q(x) W^T for a bf16 x and a quantized W; xq is space for Q(x)."""
+    rows, cols, ld = _bf16_matrix(x)
+    if cols != W.cols:
+        raise FqError(FQ_ERR_SHAPE, "fq_mx_linear")
+    if xq is None:
+        xq = MxTensor(rows, cols, FQ_MX_ROWS, x.device)
+    out, ydt, ldy = _output(out, (rows, W.rows), out_dtype or _t().float32, x.device)
+    _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref, out.data_ptr(), ydt, ldy,
+                                        _stream_ptr(stream)), "fq_mx_linear")
+    return out

@@ -475,6 +475,151 @@ fq_status fq_gemm_plain(fq_op op, const fq_qtensor* A, const fq_qtensor* B, void
   return gemm_impl(op, A, B, C, cdt, ldc, kGemmPlain, hip_stream);
 }
 
+namespace {
+constexpr int64_t kMxMaxBlocks = (int64_t)1 << 23;   // of 128 x 128: the launches count them, 256 threads each, in 32 bits
+constexpr int kMxOperandBytes = 1024, kMxScaleBytes = 256;
+
+bool mx_shape_ok(int32_t rows, int32_t cols) {
+  return rows >= 0 && cols >= 0 && ceil_div(rows, FQ_BLOCK) * ceil_div(cols, FQ_BLOCK) <= kMxMaxBlocks;
+}
+
+// bytes of codes and scales of one side, R x C
+size_t mx_codes_bytes(int32_t R, int32_t C) { return (size_t)ceil_div(R, 16) * ceil_div(C, 128) * kMxOperandBytes; }
+size_t mx_scales_bytes(int32_t R, int32_t C) { return (size_t)ceil_div(R, 64) * ceil_div(C, 128) * kMxScaleBytes; }
+
+fq_status check_mx(const fq_mx_tensor* t) {
+  if (!t) return FQ_ERR_NULL;
+  if (!mx_shape_ok(t->rows, t->cols)) return FQ_ERR_SHAPE;
+  if (!t->codes != !t->scales || !t->codes_t != !t->scales_t || (!t->codes && !t->codes_t)) return FQ_ERR_NULL;
+  if (((uintptr_t)t->codes | (uintptr_t)t->scales | (uintptr_t)t->codes_t | (uintptr_t)t->scales_t) & 15)
+    return FQ_ERR_SHAPE;
+  return FQ_OK;
+}
+
+fq::MxSide mx_side(uint8_t* codes, uint8_t* scales, int32_t R, int32_t C) {
+  return {codes, scales, (int)ceil_div(C, 128), (int)ceil_div(R, 16), (int)ceil_div(R, 64)};
+}
+fq::MxSide mx_rows(const fq_mx_tensor* t) { return mx_side(t->codes, t->scales, t->rows, t->cols); }
+fq::MxSide mx_cols(const fq_mx_tensor* t) { return mx_side(t->codes_t, t->scales_t, t->cols, t->rows); }
+
+fq_status mx_quantize_impl(const void* x, int32_t rows, int32_t cols, int64_t ld, fq_mx_rule rule, bool stochastic,
+                           uint64_t seed, const fq_mx_tensor* out, void* hip_stream) {
+  const fq_status s = check_mx(out);
+  if (s != FQ_OK) return s;
+  if (rule != FQ_MX_FLOOR && rule != FQ_MX_COVER) return FQ_ERR_ENUM;
+  if (rows < 0 || cols < 0 || ld < cols || out->rows != rows || out->cols != cols) return FQ_ERR_SHAPE;
+  if (rows == 0 || cols == 0) return FQ_OK;
+  if (!x) return FQ_ERR_NULL;
+  fq::MxQuantParams p{};
+  p.x = static_cast<const uint16_t*>(x);
+  p.ld = ld; p.rows = rows; p.cols = cols;
+  p.vec_ok = bf16_vec_ok(x, ld);
+  p.bias = rule == FQ_MX_COVER ? 63 : 0;
+  p.stochastic = stochastic; p.seed = seed;
+  p.r = mx_rows(out); p.t = mx_cols(out);
+  return fq::launch_mx_quantize(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+// Validates a product and fills its parameters; an empty output is valid (M or N 0).
+fq_status prepare_mx_gemm(fq_op op, const fq_mx_tensor* A, const fq_mx_tensor* B, void* C, fq_out_dtype cdt, int64_t ldc,
+                          fq::MxGemmParams* g) {
+  fq_status s = check_mx(A);
+  if (s == FQ_OK) s = check_mx(B);
+  if (s != FQ_OK) return s;
+  if (op != FQ_OP_NT && op != FQ_OP_NN && op != FQ_OP_TN) return FQ_ERR_ENUM;
+  if (cdt != FQ_OUT_F32 && cdt != FQ_OUT_BF16) return FQ_ERR_ENUM;
+  const bool a_t = op == FQ_OP_TN, b_t = op != FQ_OP_NT;
+  if ((a_t ? A->rows : A->cols) != (b_t ? B->rows : B->cols)) return FQ_ERR_SHAPE;
+  *g = fq::MxGemmParams{};
+  g->a = a_t ? mx_cols(A) : mx_rows(A);
+  g->b = b_t ? mx_cols(B) : mx_rows(B);
+  if (!g->a.codes || !g->b.codes) return FQ_ERR_NULL;
+  g->M = a_t ? A->cols : A->rows;
+  g->N = b_t ? B->cols : B->rows;
+  if (ldc < g->N || (int64_t)g->a.quads * g->b.quads > kMxMaxBlocks) return FQ_ERR_SHAPE;
+  if (g->M == 0 || g->N == 0) return FQ_OK;
+  if (!C) return FQ_ERR_NULL;
+  g->c = C; g->ldc = ldc; g->out_bf16 = cdt == FQ_OUT_BF16;
+  g->vec_ok = ((uintptr_t)C & 15) == 0 && ldc * (g->out_bf16 ? 2 : 4) % 16 == 0;
+  return FQ_OK;
+}
+}  // namespace
+
+size_t fq_mx_bytes(int32_t rows, int32_t cols, int32_t sides) {
+  if (!mx_shape_ok(rows, cols) || sides < FQ_MX_ROWS || sides > FQ_MX_BOTH) return 0;
+  size_t n = 256;      // never 0 for a valid shape
+  if (sides & FQ_MX_ROWS) n += align256(mx_codes_bytes(rows, cols)) + align256(mx_scales_bytes(rows, cols));
+  if (sides & FQ_MX_COLS) n += align256(mx_codes_bytes(cols, rows)) + align256(mx_scales_bytes(cols, rows));
+  return n;
+}
+
+fq_status fq_mx_bind(void* base, int32_t rows, int32_t cols, int32_t sides, fq_mx_tensor* out) {
+  if (!base || !out) return FQ_ERR_NULL;
+  if (sides < FQ_MX_ROWS || sides > FQ_MX_BOTH) return FQ_ERR_ENUM;
+  if (!mx_shape_ok(rows, cols) || ((uintptr_t)base & 255)) return FQ_ERR_SHAPE;
+  uint8_t* b = static_cast<uint8_t*>(base);
+  auto take = [&](size_t bytes) { uint8_t* p = b; b += align256(bytes); return p; };
+  *out = fq_mx_tensor{rows, cols, nullptr, nullptr, nullptr, nullptr};
+  if (sides & FQ_MX_ROWS) {
+    out->codes = take(mx_codes_bytes(rows, cols));
+    out->scales = take(mx_scales_bytes(rows, cols));
+  }
+  if (sides & FQ_MX_COLS) {
+    out->codes_t = take(mx_codes_bytes(cols, rows));
+    out->scales_t = take(mx_scales_bytes(cols, rows));
+  }
+  return FQ_OK;
+}
+
+fq_status fq_mx_quantize(const void* x_bf16, int32_t rows, int32_t cols, int64_t ld, fq_mx_rule rule, fq_mx_tensor* out,
+                         void* hip_stream) {
+  return mx_quantize_impl(x_bf16, rows, cols, ld, rule, false, 0, out, hip_stream);
+}
+
+fq_status fq_mx_quantize_sr(const void* x_bf16, int32_t rows, int32_t cols, int64_t ld, uint64_t seed, fq_mx_tensor* out,
+                            void* hip_stream) {
+  return mx_quantize_impl(x_bf16, rows, cols, ld, FQ_MX_COVER, true, seed, out, hip_stream);
+}
+
+fq_status fq_mx_dequantize(const fq_mx_tensor* t, int32_t side, void* out, fq_out_dtype odt, int64_t ldo, void* hip_stream) {
+  const fq_status s = check_mx(t);
+  if (s != FQ_OK) return s;
+  if (side != FQ_MX_ROWS && side != FQ_MX_COLS) return FQ_ERR_ENUM;
+  if (odt != FQ_OUT_F32 && odt != FQ_OUT_BF16) return FQ_ERR_ENUM;
+  fq::MxDequantParams p{};
+  p.s = side == FQ_MX_COLS ? mx_cols(t) : mx_rows(t);
+  if (!p.s.codes) return FQ_ERR_NULL;
+  if (ldo < t->cols) return FQ_ERR_SHAPE;
+  if (t->rows == 0 || t->cols == 0) return FQ_OK;
+  if (!out) return FQ_ERR_NULL;
+  p.columns = side == FQ_MX_COLS;
+  p.out = out; p.ldo = ldo; p.rows = t->rows; p.cols = t->cols; p.out_bf16 = odt == FQ_OUT_BF16;
+  p.vec_ok = ((uintptr_t)out & 15) == 0 && ldo * (p.out_bf16 ? 2 : 4) % 16 == 0;
+  return fq::launch_mx_dequantize(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+fq_status fq_mx_gemm(fq_op op, const fq_mx_tensor* A, const fq_mx_tensor* B, void* C, fq_out_dtype cdt, int64_t ldc,
+                     void* hip_stream) {
+  fq::MxGemmParams g;
+  const fq_status s = prepare_mx_gemm(op, A, B, C, cdt, ldc, &g);
+  if (s != FQ_OK || g.M == 0 || g.N == 0) return s;
+  return fq::launch_mx_gemm(g, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+fq_status fq_mx_linear(const void* x_bf16, int32_t rows, int64_t ld, fq_mx_rule rule, const fq_mx_tensor* W,
+                       fq_mx_tensor* xq, void* Y, fq_out_dtype ydt, int64_t ldy, void* hip_stream) {
+  // everything is checked before the first launch
+  if (!W || !xq) return FQ_ERR_NULL;
+  fq::MxGemmParams g;
+  fq_status s = prepare_mx_gemm(FQ_OP_NT, xq, W, Y, ydt, ldy, &g);
+  if (s != FQ_OK) return s;
+  fq_mx_tensor side = *xq;       // only the rows' side is needed
+  side.codes_t = side.scales_t = nullptr;
+  s = mx_quantize_impl(x_bf16, rows, W->cols, ld, rule, false, 0, &side, hip_stream);
+  if (s != FQ_OK || g.M == 0 || g.N == 0) return s;
+  return fq::launch_mx_gemm(g, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
 fq_status fq_gemm_tile_plan(int32_t rows_out, int32_t cols_out, int32_t compute_units,
                             int32_t plan[3]) {
   if (!plan) return FQ_ERR_NULL;

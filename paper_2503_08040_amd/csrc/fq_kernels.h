@@ -130,6 +130,48 @@ struct RmsParams {
   int vec_w;           // so does w
 };
 
+// Microscaled 4-bit matrices.  One side of a matrix: R x C elements with the contraction along C, strips of 16 rows
+// times nkb = ceil(C / 128) operands of 1 KiB; scales 256 bytes per 64 rows and 128 columns.
+struct MxSide {
+  uint8_t* codes;      // nullptr: not kept
+  uint8_t* scales;
+  int nkb, strips, quads;   // ceil(C / 128), ceil(R / 16), ceil(R / 64)
+};
+
+struct MxQuantParams {
+  const uint16_t* x;   // bf16 bits, row-major [rows, ld]
+  int64_t ld;
+  int rows, cols;
+  int vec_ok;          // 16-byte loads
+  int bias;            // added to a group's largest bf16 magnitude before its exponent is taken: 0 FLOOR, 63 COVER
+  int stochastic;
+  uint64_t seed;
+  MxSide r, t;         // along the rows, along the columns
+};
+
+struct MxDequantParams {
+  MxSide s;
+  int columns;         // which side s is
+  void* out;           // row-major [rows, ldo]
+  int64_t ldo;
+  int rows, cols;
+  int vec_ok;          // 16-byte stores
+  int out_bf16;
+};
+
+struct MxGemmParams {
+  MxSide a, b;         // C[i, j] = sum over k of a[i, k] b[j, k]
+  void* c;
+  int64_t ldc;
+  int M, N;
+  int out_bf16;
+  int vec_ok;          // C's base and pitch allow 16-byte stores
+};
+
+hipError_t launch_mx_quantize(const MxQuantParams& p, hipStream_t st);
+hipError_t launch_mx_dequantize(const MxDequantParams& p, hipStream_t st);
+hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st);
+
 hipError_t launch_quantize(const QuantParams& p, hipStream_t st);
 hipError_t launch_untile(const int8_t* tiled, int rows, int cols, int8_t* dense, hipStream_t st);
 hipError_t launch_gemm(const GemmParams& p, bool debug, hipStream_t st);

@@ -1,0 +1,329 @@
+// Microscaled 4-bit matrices: quantization along the rows, the columns or both from one read of x, and the way back.
+//
+// A group of 32 values shares 2^s; s comes from the exponent of the group's largest magnitude, which is an integer
+// maximum over the bf16 bits without the sign (so infinities and NaNs come out largest), and the codes from the
+// conversion instructions, which divide by a power of two and round to E2M1 to nearest even.  Both kernels stream:
+// 2 bytes an element on the bf16 side, 17/32 per side on the other.
+//
+// A wavefront has 32 rows x 128 columns, a lane 8 x 8 of them: 16 lanes read 256 bytes of a row, four lanes next to
+// each other hold a row's group, the four lanes 16 apart a column's.  So either maximum is taken in registers with
+// two exchanges, and neither side needs the elements transposed through LDS; only the finished codes pass through it,
+// to leave in 16-byte stores.
+#include "fq_device.h"
+#include "fq_kernels.h"
+
+namespace fq {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTile = 128;        // rows and columns of a workgroup: whole operands along either axis
+constexpr int kWaveRows = 32;     // of a wavefront: one group along the columns
+constexpr int kOperand = 1024;    // 16 rows x 128
+constexpr int kScaleBlock = 256;  // scales of 64 rows x 128
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint16_t v2h __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2h, a), __builtin_bit_cast(v2h, b)));
+}
+
+// maximum over the 4 lanes of a quad
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = pk_max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lanes 1, 0, 3, 2
+  return pk_max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // lanes 2, 3, 0, 1
+}
+
+// maximum over the 4 lanes 16 apart
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v2u s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  v = pk_max(s[0], s[1]);
+  s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return pk_max(s[0], s[1]);
+}
+
+// Scale byte of a group with largest magnitude m (bf16 bits without the sign).  bias 63 takes the next exponent if
+// the mantissa is above 1.5; the smallest byte is 0.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t m, int bias) {
+  const uint32_t e = (m + (uint32_t)bias) >> 7;
+  return m >= 0x7F80u ? 255u : (e > 2u ? e : 2u) - 2u;
+}
+
+// 2^(byte - 127) as the conversions take it; 2^-127 is a subnormal number.
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+
+// 2^(127 - byte): multiplication by it divides by the scale.
+__device__ __forceinline__ float scale_inverse(uint32_t byte) {
+  return __uint_as_float(byte < 254u ? (254u - byte) << 23 : 0x00400000u);
+}
+
+__device__ __forceinline__ uint32_t cvt_fp4(uint32_t old, uint32_t pair, float scale, int sel) {
+  const v2bf v = __builtin_bit_cast(v2bf, pair);
+  switch (sel) {
+    case 0: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 3);
+  }
+}
+
+// Stochastic code of a bf16 value (bits) with 16 random bits: t = |x| / 2^s in units of 2^-17, the step above it is
+// 2^16, 2^17 or 2^18 of them; the sum of t and the random part of a step is cut to whole steps.  A finite group has
+// t <= 6; the minimum is for the others, whose code is dropped.
+__device__ __forceinline__ uint32_t code_sr(uint32_t bits, uint32_t u, float inv) {
+  const float x = __uint_as_float((bits & 0x7FFFu) << 16);
+  const uint32_t t = (uint32_t)fminf(x * inv * 0x1p17f, 0x1p20f);      // the conversion cuts
+  const uint32_t sh = (t >= 1u << 18) + (t >= 1u << 19);
+  const uint32_t q = (t + (u << sh)) >> (16 + sh);     // whole steps: codes 0-4 at sh 0, 4 + q - 2 at 1, 6 + q - 2 at 2
+  return (q + 2u * sh) | ((bits >> 12) & 8u);
+}
+
+struct Random8 { uint32_t w[4]; };
+
+template <bool kRows, bool kCols, bool kSr>
+__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) {
+  __shared__ __attribute__((aligned(16))) uint8_t codes_lds[4][2][2 * kOperand];   // wavefront, side
+  __shared__ __attribute__((aligned(16))) uint8_t scales_lds[2][2][kScaleBlock];   // side, half of the tile
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int h = lane >> 4, q = lane & 15;
+  const int nbc = p.r.nkb;                               // tiles across
+  const int bi = blockIdx.x / nbc, bk = blockIdx.x % nbc;
+  const int row0 = bi * kTile + w * kWaveRows + 8 * h, col0 = bk * kTile + 8 * q;
+
+  v4u x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + i;
+    x[i] = v4u{0u, 0u, 0u, 0u};
+    if (row < p.rows && col0 < p.cols) {
+      const uint16_t* src = p.x + row * p.ld + col0;
+      if (p.vec_ok && col0 + 8 <= p.cols) {
+        x[i] = *reinterpret_cast<const v4u*>(src);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col0 + e < p.cols) x[i][e >> 1] |= (uint32_t)src[e] << (16 * (e & 1));
+      }
+    }
+  }
+  Random8 rnd[kSr ? 8 : 1];
+  if constexpr (kSr) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      philox4x32_10((uint32_t)(col0 >> 3), (uint32_t)(row0 + i), (uint32_t)p.seed, (uint32_t)(p.seed >> 32), rnd[i].w);
+  }
+  constexpr uint32_t kMag = 0x7FFF7FFFu;
+
+  if constexpr (kRows) {
+    uint8_t* const lds = codes_lds[w][0];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      // rows i and i + 1: their maxima in the two halves of a dword
+      uint32_t m2[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        m2[k] = pk_max(pk_max(x[i + k][0] & kMag, x[i + k][1] & kMag), pk_max(x[i + k][2] & kMag, x[i + k][3] & kMag));
+      const uint32_t m = quad_max(pk_max(__builtin_amdgcn_perm(m2[1], m2[0], 0x05040100u),
+                                         __builtin_amdgcn_perm(m2[1], m2[0], 0x07060302u)));
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t byte = scale_byte(k ? m >> 16 : m & 0xFFFFu, p.bias);
+        uint32_t c = 0;
+        if constexpr (kSr) {
+          const float inv = scale_inverse(byte);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            c |= code_sr((x[i + k][e >> 1] >> (16 * (e & 1))) & 0xFFFFu, (rnd[i + k].w[e >> 1] >> (16 * (e & 1))) & 0xFFFFu,
+                         inv) << (4 * e);
+        } else {
+          const float s = scale_value(byte);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) c = cvt_fp4(c, x[i + k][d], s, d);
+        }
+        if (byte == 255u) c = 0;
+        const int r = 8 * h + i + k;                     // of the 32
+        *reinterpret_cast<uint32_t*>(lds + (r >> 4) * kOperand + ((r & 15) + 16 * (q >> 2)) * 16 + 4 * (q & 3)) = c;
+        if ((q & 3) == 0)
+          scales_lds[0][w >> 1][((r & 15) + 16 * (q >> 2)) * 4 + 2 * (w & 1) + (r >> 4)] = (uint8_t)byte;
+      }
+    }
+  }
+  if constexpr (kCols) {
+    uint8_t* const lds = codes_lds[w][1];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {                        // columns 2 d and 2 d + 1 of the lane's 8
+      uint32_t m = x[0][d] & kMag;
+#pragma unroll
+      for (int i = 1; i < 8; ++i) m = pk_max(m, x[i][d] & kMag);
+      m = row_max(m);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t byte = scale_byte(k ? m >> 16 : m & 0xFFFFu, p.bias);
+        uint32_t c = 0;
+        if constexpr (kSr) {
+          const float inv = scale_inverse(byte);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            c |= code_sr((x[i][d] >> (16 * k)) & 0xFFFFu, (rnd[i].w[d] >> (16 * k)) & 0xFFFFu, inv) << (4 * i);
+        } else {
+          const float s = scale_value(byte);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            c = cvt_fp4(c, __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], k ? 0x07060302u : 0x05040100u), s, i);
+        }
+        if (byte == 255u) c = 0;
+        const int col = 8 * q + 2 * d + k;               // of the tile's 128
+        *reinterpret_cast<uint32_t*>(lds + col * 16 + 4 * h) = c;
+        if (h == 0) scales_lds[1][col >> 6][((col & 15) + 16 * w) * 4 + ((col >> 4) & 3)] = (uint8_t)byte;
+      }
+    }
+  }
+  __syncthreads();
+
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    if constexpr (kRows) {
+      const int strip = bi * 8 + w * 2 + u;
+      if (strip < p.r.strips)
+        *reinterpret_cast<v4u*>(p.r.codes + ((int64_t)strip * p.r.nkb + bk) * kOperand + lane * 16) =
+            *reinterpret_cast<const v4u*>(codes_lds[w][0] + u * kOperand + lane * 16);
+    }
+    if constexpr (kCols) {
+      const int c = lane + 64 * u, strip = bk * 8 + (c >> 4);
+      if (strip < p.t.strips)
+        *reinterpret_cast<v4u*>(p.t.codes + ((int64_t)strip * p.t.nkb + bi) * kOperand + w * 256 + (c & 15) * 16) =
+            *reinterpret_cast<const v4u*>(codes_lds[w][1] + c * 16);
+    }
+  }
+  const int half = w & 1;
+  if (kRows && w < 2 && 2 * bi + half < p.r.quads)
+    *reinterpret_cast<uint32_t*>(p.r.scales + ((int64_t)(2 * bi + half) * p.r.nkb + bk) * kScaleBlock + lane * 4) =
+        *reinterpret_cast<const uint32_t*>(&scales_lds[0][half][lane * 4]);
+  if (kCols && w >= 2 && 2 * bk + half < p.t.quads)
+    *reinterpret_cast<uint32_t*>(p.t.scales + ((int64_t)(2 * bk + half) * p.t.nkb + bi) * kScaleBlock + lane * 4) =
+        *reinterpret_cast<const uint32_t*>(&scales_lds[1][half][lane * 4]);
+}
+
+__device__ __forceinline__ uint32_t cvt_bf16(uint32_t codes, float scale, int sel) {
+  v2bf v;
+  switch (sel) {
+    case 0: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0); break;
+    case 1: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1); break;
+    case 2: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2); break;
+    default: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3); break;
+  }
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// The same split of a tile the other way: a lane takes 8 dwords of codes (8 values each) and has 8 x 8 values.
+template <bool kCols, bool kBf16>
+__global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxDequantParams p) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int h = lane >> 4, q = lane & 15;
+  const int nbc = (p.cols + kTile - 1) / kTile;
+  const int bi = blockIdx.x / nbc, bk = blockIdx.x % nbc;
+  const int row0 = bi * kTile + w * kWaveRows + 8 * h, col0 = bk * kTile + 8 * q;
+  if (row0 >= p.rows || col0 >= p.cols) return;
+  constexpr uint32_t kNan = 0x7FC07FC0u;
+  uint32_t y[8][4];          // bf16 pairs
+  if constexpr (!kCols) {
+    const int strip = row0 >> 4, r = row0 & 15;          // the lane's 8 rows lie in one strip
+    const int64_t at = (int64_t)strip * p.s.nkb + bk;
+    const int64_t sat = (int64_t)(strip >> 2) * p.s.nkb + bk;
+    uint32_t c[8], byte[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      c[i] = *reinterpret_cast<const uint32_t*>(p.s.codes + at * kOperand + (r + i + 16 * (q >> 2)) * 16 + 4 * (q & 3));
+      byte[i] = p.s.scales[sat * kScaleBlock + (r + i + 16 * (q >> 2)) * 4 + (strip & 3)];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) y[i][d] = byte[i] == 255u ? kNan : cvt_bf16(c[i], scale_value(byte[i]), d);
+  } else {
+    const int strip = col0 >> 4, r = col0 & 15;
+    const int64_t at = (int64_t)strip * p.s.nkb + bi;
+    const int64_t sat = (int64_t)(strip >> 2) * p.s.nkb + bi;
+    uint32_t c[8], byte[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      c[j] = *reinterpret_cast<const uint32_t*>(p.s.codes + at * kOperand + (r + j + 16 * w) * 16 + 4 * h);
+      byte[j] = p.s.scales[sat * kScaleBlock + (r + j + 16 * w) * 4 + (strip & 3)];
+    }
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // rows 2 i and 2 i + 1 of columns 2 d and 2 d + 1
+        uint32_t v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          v[k] = byte[2 * d + k] == 255u ? kNan : cvt_bf16(c[2 * d + k], scale_value(byte[2 * d + k]), i);
+        y[2 * i][d] = __builtin_amdgcn_perm(v[1], v[0], 0x05040100u);
+        y[2 * i + 1][d] = __builtin_amdgcn_perm(v[1], v[0], 0x07060302u);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (row0 + i >= p.rows) break;
+    const int64_t o = (row0 + i) * p.ldo + col0;
+    const bool whole = p.vec_ok && col0 + 8 <= p.cols;
+    if constexpr (kBf16) {
+      uint16_t* dst = static_cast<uint16_t*>(p.out) + o;
+      if (whole) {
+        *reinterpret_cast<v4u*>(dst) = v4u{y[i][0], y[i][1], y[i][2], y[i][3]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col0 + e < p.cols) dst[e] = (uint16_t)(y[i][e >> 1] >> (16 * (e & 1)));
+      }
+    } else {
+      uint32_t* dst = static_cast<uint32_t*>(p.out) + o;
+      if (whole) {
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+          reinterpret_cast<v4u*>(dst)[d] = v4u{y[i][2 * d] << 16, y[i][2 * d] & 0xFFFF0000u, y[i][2 * d + 1] << 16,
+                                               y[i][2 * d + 1] & 0xFFFF0000u};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col0 + e < p.cols) dst[e] = (e & 1) ? y[i][e >> 1] & 0xFFFF0000u : y[i][e >> 1] << 16;
+      }
+    }
+  }
+}
+
+int tiles(int rows, int cols) { return ((rows + kTile - 1) / kTile) * ((cols + kTile - 1) / kTile); }
+
+template <bool kSr>
+void quantize_sides(const MxQuantParams& p, dim3 grid, hipStream_t st) {
+  if (p.r.codes && p.t.codes) hipLaunchKernelGGL((mx_quantize_kernel<true, true, kSr>), grid, dim3(kThreads), 0, st, p);
+  else if (p.r.codes) hipLaunchKernelGGL((mx_quantize_kernel<true, false, kSr>), grid, dim3(kThreads), 0, st, p);
+  else hipLaunchKernelGGL((mx_quantize_kernel<false, true, kSr>), grid, dim3(kThreads), 0, st, p);
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const MxQuantParams& p, hipStream_t st) {
+  const dim3 grid(tiles(p.rows, p.cols));
+  if (p.stochastic) quantize_sides<true>(p, grid, st);
+  else quantize_sides<false>(p, grid, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_dequantize(const MxDequantParams& p, hipStream_t st) {
+  const dim3 grid(tiles(p.rows, p.cols)), block(kThreads);
+  if (p.columns) {
+    if (p.out_bf16) hipLaunchKernelGGL((mx_dequantize_kernel<true, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((mx_dequantize_kernel<true, false>), grid, block, 0, st, p);
+  } else {
+    if (p.out_bf16) hipLaunchKernelGGL((mx_dequantize_kernel<false, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((mx_dequantize_kernel<false, false>), grid, block, 0, st, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace fq

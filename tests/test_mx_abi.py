@@ -1,0 +1,159 @@
+"""Host-side checks of the microscaled calls that need no GPU: sizes, binding, and what is refused before anything is
+launched; what the Python layer hands over and refuses."""
+import ctypes as C
+import types
+
+import pytest
+import torch
+
+import paper_2503_08040_amd as fq
+
+X = C.c_void_p(0x2000)
+
+
+def _side(R, Cc):
+    up = lambda n: -(-n // 256) * 256
+    return up(-(-R // 16) * -(-Cc // 128) * 1024) + up(-(-R // 64) * -(-Cc // 128) * 256)
+
+
+def test_bytes():
+    for R, Cc in [(0, 0), (0, 7), (1, 1), (16, 128), (17, 129), (300, 70)]:
+        assert fq.fq_mx_bytes(R, Cc, fq.FQ_MX_ROWS) == 256 + _side(R, Cc)
+        assert fq.fq_mx_bytes(R, Cc, fq.FQ_MX_COLS) == 256 + _side(Cc, R)
+        assert fq.fq_mx_bytes(R, Cc, fq.FQ_MX_BOTH) == 256 + _side(R, Cc) + _side(Cc, R)
+    for bad in [(-1, 5, 1), (5, -1, 1), (5, 5, 0), (5, 5, 4), (5, 5, -1)]:
+        assert fq.fq_mx_bytes(*bad) == 0
+    most = 2 ** 23 * 128
+    assert fq.fq_mx_bytes(1, most) > 0 and fq.fq_mx_bytes(1, most + 1) == 0 == fq.fq_mx_bytes(most + 1, 1)
+    assert fq.fq_mx_bytes(2 ** 31 - 1, 2 ** 31 - 1, 3) == 0
+
+
+def _bind(rows, cols, sides=fq.FQ_MX_BOTH, base=0x100000):
+    t = fq.fq_mx_tensor()
+    assert fq.lib().fq_mx_bind(C.c_void_p(base), rows, cols, sides, C.byref(t)) == fq.FQ_OK
+    return t
+
+
+def test_bind():
+    t = _bind(130, 200)
+    assert (t.rows, t.cols) == (130, 200)
+    ptrs = [t.codes, t.scales, t.codes_t, t.scales_t]
+    assert all(p % 256 == 0 for p in ptrs) and sorted(set(ptrs)) == ptrs and ptrs[0] == 0x100000
+    assert t.scales_t + 4 * 2 * 256 <= 0x100000 + fq.fq_mx_bytes(130, 200, 3)
+    r, c = _bind(130, 200, fq.FQ_MX_ROWS), _bind(130, 200, fq.FQ_MX_COLS)
+    assert r.codes and r.scales and not r.codes_t and not r.scales_t
+    assert c.codes_t and c.scales_t and not c.codes and not c.scales
+    bind, out = fq.lib().fq_mx_bind, C.byref(fq.fq_mx_tensor())
+    assert bind(None, 4, 4, 1, out) == bind(X, 4, 4, 1, None) == fq.FQ_ERR_NULL
+    assert bind(X, 4, 4, 0, out) == bind(X, 4, 4, 4, out) == fq.FQ_ERR_ENUM
+    assert bind(C.c_void_p(0x2010), 4, 4, 1, out) == bind(X, -4, 4, 1, out) == bind(X, 1, 2 ** 31 - 1, 1, out) == fq.FQ_ERR_SHAPE
+
+
+def test_quantize_refusals():
+    t = _bind(256, 200)
+    L, r = fq.lib(), C.byref(t)
+    for call in (lambda x, m, n, ld, out, rule=0: L.fq_mx_quantize(x, m, n, ld, rule, out, None),
+                 lambda x, m, n, ld, out, rule=0: L.fq_mx_quantize_sr(x, m, n, ld, 7, out, None)):
+        assert call(X, 256, 200, 200, None) == call(None, 256, 200, 200, r) == fq.FQ_ERR_NULL
+        for m, n, ld in [(256, 200, 199), (-1, 200, 200), (256, -1, 200), (255, 200, 200), (256, 201, 201)]:
+            assert call(X, m, n, ld, r) == fq.FQ_ERR_SHAPE
+    assert L.fq_mx_quantize(X, 256, 200, 200, 2, r, None) == fq.FQ_ERR_ENUM
+    assert L.fq_mx_quantize(X, 256, 200, 200, -1, r, None) == fq.FQ_ERR_ENUM
+    for field, value, want in [("codes", None, fq.FQ_ERR_NULL), ("scales", None, fq.FQ_ERR_NULL),
+                               ("scales_t", None, fq.FQ_ERR_NULL), ("codes_t", 0x100008, fq.FQ_ERR_SHAPE),
+                               ("rows", -1, fq.FQ_ERR_SHAPE), ("cols", 2 ** 31 - 1, fq.FQ_ERR_SHAPE)]:
+        b = _bind(256, 200)
+        setattr(b, field, value)
+        assert L.fq_mx_quantize(X, 256, 200, 200, 0, C.byref(b), None) == want, field
+    none = fq.fq_mx_tensor(rows=4, cols=4)
+    assert L.fq_mx_quantize(X, 4, 4, 4, 0, C.byref(none), None) == fq.FQ_ERR_NULL
+    for rows, cols in [(0, 5), (5, 0), (0, 0)]:
+        assert L.fq_mx_quantize(None, rows, cols, cols, 0, C.byref(_bind(rows, cols)), None) == fq.FQ_OK
+
+
+def test_dequantize_refusals():
+    L, t = fq.lib(), _bind(40, 50)
+    d = lambda t, side, out, odt=0, ldo=50: L.fq_mx_dequantize(C.byref(t) if t else None, side, out, odt, ldo, None)
+    assert d(None, 1, X) == d(t, 1, None) == fq.FQ_ERR_NULL
+    assert d(t, 0, X) == d(t, 3, X) == d(t, 1, X, 2) == d(t, 1, X, -1) == fq.FQ_ERR_ENUM
+    assert d(t, 1, X, 0, 49) == fq.FQ_ERR_SHAPE
+    assert d(_bind(40, 50, fq.FQ_MX_COLS), fq.FQ_MX_ROWS, X) == d(_bind(40, 50, 1), fq.FQ_MX_COLS, X) == fq.FQ_ERR_NULL
+    assert d(_bind(0, 50), 1, None) == d(_bind(40, 0), 2, None, 1, 0) == fq.FQ_OK
+
+
+def test_gemm_refusals():
+    L = fq.lib()
+    ref = lambda t: C.byref(t) if t is not None else None
+    g = lambda op, a, b, c=X, cdt=0, ldc=384: L.fq_mx_gemm(op, ref(a), ref(b), c, cdt, ldc, None)
+    a, b = _bind(256, 512), _bind(384, 512)
+    assert g(0, None, b) == g(0, a, None) == g(0, a, b, None) == fq.FQ_ERR_NULL
+    assert g(3, a, b) == g(-1, a, b) == g(0, a, b, cdt=2) == g(0, a, b, cdt=-1) == fq.FQ_ERR_ENUM
+    assert g(0, a, b, ldc=383) == g(0, a, _bind(384, 640)) == g(1, a, b, ldc=512) == g(2, a, b, ldc=512) == fq.FQ_ERR_SHAPE
+    rows, cols = fq.FQ_MX_ROWS, fq.FQ_MX_COLS
+    for op, sa, sb in [(0, cols, rows), (0, rows, cols), (1, cols, cols), (1, rows, rows), (2, rows, cols), (2, cols, rows)]:
+        shape = {0: ((64, 32), (96, 32)), 1: ((64, 32), (32, 96)), 2: ((32, 64), (32, 96))}[op]
+        assert g(op, _bind(*shape[0], sa), _bind(*shape[1], sb)) == fq.FQ_ERR_NULL, (op, sa, sb)
+    wide = _bind(2 ** 18, 1, rows), _bind(2 ** 18 + 64, 1, rows)       # 2^12 and 2^12 + 1 tiles of 64
+    assert g(0, *wide, ldc=2 ** 19) == fq.FQ_ERR_SHAPE
+    assert g(0, _bind(0, 512), b, None) == g(0, a, _bind(0, 512), None, ldc=0) == fq.FQ_OK
+
+
+def test_linear_refusals():
+    L = fq.lib()
+    ref = lambda t: C.byref(t) if t is not None else None
+    f = lambda w, q, x=X, rows=40, ld=512, rule=0, y=X, ydt=0, ldy=384: \
+        L.fq_mx_linear(x, rows, ld, rule, ref(w), ref(q), y, ydt, ldy, None)
+    w, q = _bind(384, 512), _bind(40, 512)
+    assert f(None, q) == f(w, None) == f(w, q, x=None) == f(w, q, y=None) == fq.FQ_ERR_NULL
+    assert f(w, q, rule=2) == f(w, q, ydt=2) == fq.FQ_ERR_ENUM
+    assert f(w, q, rows=41) == f(w, q, rows=-1) == f(w, q, ld=511) == f(w, q, ldy=383) == f(w, _bind(40, 513)) == fq.FQ_ERR_SHAPE
+    assert f(_bind(384, 512, fq.FQ_MX_COLS), q) == f(w, _bind(40, 512, fq.FQ_MX_COLS)) == fq.FQ_ERR_NULL
+    assert f(w, _bind(0, 512), x=None, rows=0, y=None) == fq.FQ_OK
+
+
+class _Recorder:
+    def __init__(self):
+        self.calls = []
+        self.fq_status_string = fq.lib().fq_status_string
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return fq.FQ_OK
+        return call
+
+
+def test_python_layer(monkeypatch):
+    """Shapes, pitches, types and sides as they reach the library; what the Python functions refuse by themselves."""
+    lib = fq.lib()
+    rec = _Recorder()
+    stream = types.SimpleNamespace(cuda_stream=5)
+    tensor = lambda rows, cols, sides=3: fq.MxTensor(rows, cols, sides, device="cpu")
+    q, w, g = tensor(4, 32), tensor(6, 32), tensor(4, 6)
+    x = types.SimpleNamespace(dtype=torch.bfloat16, is_cuda=True, shape=(4, 32), dim=lambda: 2, device="cpu",
+                              stride=lambda: (40, 1), data_ptr=lambda: 256)
+    monkeypatch.setattr(fq, "_lib", rec)
+    fq.fq_mx_quantize(x, out=q, rule=fq.FQ_MX_COVER, stream=stream)
+    fq.fq_mx_quantize_sr(x, 2 ** 40 + 1, out=q, stream=stream)
+    name, args = rec.calls[0]
+    assert name == "fq_mx_quantize" and args[:5] == (256, 4, 32, 40, 1) and args[-1] == 5
+    assert rec.calls[1][1][4].value == 2 ** 40 + 1
+    x.dtype = torch.float32
+    with pytest.raises(AssertionError):
+        fq.fq_mx_quantize(x, out=q, stream=stream)
+    x.dtype, x.shape = torch.bfloat16, (4, 33)
+    with pytest.raises(fq.FqError):
+        fq.fq_mx_linear(x, w, stream=stream)
+    for bad in (torch.empty((4, 6)), torch.empty((6, 4))):          # not on the GPU, wrong shape
+        with pytest.raises(AssertionError):
+            fq.fq_mx_gemm(fq.FQ_OP_NT, q, w, out=bad, stream=stream)
+    with pytest.raises(fq.FqError):
+        fq.fq_mx_gemm(7, q, w, stream=stream)
+    assert len(rec.calls) == 2
+    monkeypatch.setattr(fq, "_lib", lib)
+    assert q.view("codes").shape == (1, 1, 1024) and q.view("scales_t").shape == (1, 1, 256)
+    assert q.view("codes_t").shape == (2, 1, 1024) and tensor(4, 4, 1).view("codes_t") is None
+    assert g.view("codes").data_ptr() == g.c.codes
+    for bad in [(-1, 4, 1), (4, 4, 0), (4, 4, 4)]:
+        with pytest.raises(fq.FqError):
+            tensor(*bad)
