@@ -522,13 +522,30 @@ fq_status fq_mx_dequantize(const fq_mx_tensor *t, int32_t side, void *out, fq_ou
 fq_status fq_mx_gemm(fq_op op, const fq_mx_tensor *A, const fq_mx_tensor *B, void *C, fq_out_dtype cdt,
                      int64_t ldc, void *hip_stream);
 
+/* The tiles that a product is cut into. */
+typedef enum fq_mx_form {
+  FQ_MX_FORM_32x32 = 0,
+  FQ_MX_FORM_32x64 = 1,
+  FQ_MX_FORM_64x64 = 2,
+  FQ_MX_FORM_128x128 = 3,
+  FQ_MX_FORM_256x256 = 4
+} fq_mx_form;
+
+/* form[0]: the tiles of fq_mx_gemm for a rows_out x cols_out output and a contraction of that length (an fq_mx_form, 0
+ * for an empty output); form[1]: 1 if fq_mx_linear computes that output in one launch.  Host-only inspection,
+ * compute_units as for fq_gemm_tile_plan. */
+fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contraction, int32_t compute_units,
+                          int32_t form[2]);
+
 /*
  * Forward of a linear layer: Y = Q(X) W^T with X [rows, ld] in bf16, quantized along its rows by
  * `rule`, and W quantized before (rows' side, [N, K], K = X's columns).  The same values, bit for
- * bit, as fq_mx_quantize into `xq` and fq_mx_gemm.  xq: a tensor of X's shape that keeps its rows'
- * side; overwritten, its contents are unspecified afterwards.
+ * bit, as fq_mx_quantize into `xq` and fq_mx_gemm; for few rows in one launch that quantizes X on
+ * its way into the product.  xq: a tensor of X's shape that keeps its rows' side, whose contents
+ * are unspecified afterwards; up to FQ_MX_LINEAR_ROWS rows it may be NULL.
  * Errors as those two calls.
  */
+#define FQ_MX_LINEAR_ROWS 16
 fq_status fq_mx_linear(const void *x_bf16, int32_t rows, int64_t ld, fq_mx_rule rule, const fq_mx_tensor *W,
                        fq_mx_tensor *xq, void *Y, fq_out_dtype ydt, int64_t ldy, void *hip_stream);
 

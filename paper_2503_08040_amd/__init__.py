@@ -25,8 +25,10 @@ FQ_OP_NT, FQ_OP_NN, FQ_OP_TN = 0, 1, 2
 FQ_OUT_F32, FQ_OUT_BF16 = 0, 1
 FQ_TILES_256x256, FQ_TILES_32x32, FQ_TILES_128x64, FQ_TILES_128x128 = 0, 1, 2, 3
 FQ_MX_GROUP = 32
+FQ_MX_LINEAR_ROWS = 16
 FQ_MX_ROWS, FQ_MX_COLS, FQ_MX_BOTH = 1, 2, 3
 FQ_MX_FLOOR, FQ_MX_COVER = 0, 1
+FQ_MX_FORM_32x32, FQ_MX_FORM_32x64, FQ_MX_FORM_64x64, FQ_MX_FORM_128x128, FQ_MX_FORM_256x256 = 0, 1, 2, 3, 4
 FQ_FORM_256x256, FQ_FORM_32x32, FQ_FORM_128x64, FQ_FORM_128x128, FQ_FORM_LOADERS_128x64, FQ_FORM_LOADERS_128x128, \
     FQ_FORM_LOADERS_128x256 = 0, 1, 2, 3, 4, 5, 6
 
@@ -42,7 +44,7 @@ EXPORTS = ["fq_qtensor_bytes", "fq_qtensor_bind", "fq_quantize", "fq_quantize_sr
            "fq_glu_forward", "fq_glu_backward", "fq_rmsnorm_forward",
            "fq_rmsnorm_backward", "fq_rmsnorm_backward_static",
            "fq_mx_bytes", "fq_mx_bind", "fq_mx_quantize", "fq_mx_quantize_sr", "fq_mx_dequantize", "fq_mx_gemm",
-           "fq_mx_linear"]
+           "fq_mx_gemm_form", "fq_mx_linear"]
 
 
 class fq_qtensor(C.Structure):
@@ -161,6 +163,8 @@ def lib():
         L.fq_mx_dequantize.argtypes = [mx, C.c_int32, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]
         L.fq_mx_gemm.restype = C.c_int
         L.fq_mx_gemm.argtypes = [C.c_int, mx, mx, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]
+        L.fq_mx_gemm_form.restype = C.c_int
+        L.fq_mx_gemm_form.argtypes = [C.c_int32] * 4 + [C.POINTER(C.c_int32)]
         L.fq_mx_linear.restype = C.c_int
         L.fq_mx_linear.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int, mx, mx, C.c_void_p, C.c_int, C.c_int64,
                                    C.c_void_p]
@@ -671,14 +675,23 @@ def fq_mx_gemm(op, A: MxTensor, B: MxTensor, out=None, out_dtype=None, stream=No
     return out
 
 
+def fq_mx_gemm_form(rows_out, cols_out, contraction, compute_units=0):
+    """(FQ_MX_FORM_* of fq_mx_gemm, whether fq_mx_linear is one launch) for an output and a contraction."""
+    out = (C.c_int32 * 2)()
+    _check(lib().fq_mx_gemm_form(int(rows_out), int(cols_out), int(contraction), int(compute_units), out),
+           "fq_mx_gemm_form")
+    return int(out[0]), bool(out[1])
+
+
 def fq_mx_linear(x, W: MxTensor, xq: MxTensor = None, rule=FQ_MX_FLOOR, out=None, out_dtype=None, stream=None):
-    """Y = Q(x) W^T for a bf16 x and a quantized W; xq is space for Q(x)."""
+    """Y = Q(x) W^T for a bf16 x and a quantized W; xq is space for Q(x), taken if x has more than FQ_MX_LINEAR_ROWS rows
+    and none is given."""
     rows, cols, ld = _bf16_matrix(x)
     if cols != W.cols:
         raise FqError(FQ_ERR_SHAPE, "fq_mx_linear")
-    if xq is None:
+    if xq is None and rows > FQ_MX_LINEAR_ROWS:
         xq = MxTensor(rows, cols, FQ_MX_ROWS, x.device)
     out, ydt, ldy = _output(out, (rows, W.rows), out_dtype or _t().float32, x.device)
-    _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref, out.data_ptr(), ydt, ldy,
-                                        _stream_ptr(stream)), "fq_mx_linear")
+    _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref if xq else None, out.data_ptr(), ydt,
+                                        ldy, _stream_ptr(stream)), "fq_mx_linear")
     return out

@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfq.so")
 HEADER = os.path.join(HERE, "..", "include", "fq.h")
 SOURCES = ["fq_api.hip", "fq_quantize.hip", "fq_gemm.hip", "fq_gemm_tile.hip", "fq_gemm_ring.hip", "fq_group.hip", "fq_ctx.hip", "fq_mx.hip", "fq_mx_gemm.hip"]
-HEADERS = ["fq_device.h", "fq_gemm_unit.h", "fq_kernels.h", os.path.join("..", "..", "include", "fq.h")]
+HEADERS = ["fq_device.h", "fq_mx_device.h", "fq_gemm_unit.h", "fq_kernels.h", os.path.join("..", "..", "include", "fq.h")]
 
 # Packed FP32 VALU instructions are switched off for the device pass (the host
 # pass prints a harmless "not a recognized feature" note).

@@ -502,22 +502,21 @@ fq::MxSide mx_side(uint8_t* codes, uint8_t* scales, int32_t R, int32_t C) {
 fq::MxSide mx_rows(const fq_mx_tensor* t) { return mx_side(t->codes, t->scales, t->rows, t->cols); }
 fq::MxSide mx_cols(const fq_mx_tensor* t) { return mx_side(t->codes_t, t->scales_t, t->cols, t->rows); }
 
-fq_status mx_quantize_impl(const void* x, int32_t rows, int32_t cols, int64_t ld, fq_mx_rule rule, bool stochastic,
-                           uint64_t seed, const fq_mx_tensor* out, void* hip_stream) {
+// Validates a quantization and fills its parameters; x is null in them if there is nothing to do.
+fq_status prepare_mx_quantize(const void* x, int32_t rows, int32_t cols, int64_t ld, fq_mx_rule rule,
+                              const fq_mx_tensor* out, fq::MxQuantParams* p) {
   const fq_status s = check_mx(out);
   if (s != FQ_OK) return s;
   if (rule != FQ_MX_FLOOR && rule != FQ_MX_COVER) return FQ_ERR_ENUM;
   if (rows < 0 || cols < 0 || ld < cols || out->rows != rows || out->cols != cols) return FQ_ERR_SHAPE;
+  *p = fq::MxQuantParams{};
   if (rows == 0 || cols == 0) return FQ_OK;
   if (!x) return FQ_ERR_NULL;
-  fq::MxQuantParams p{};
-  p.x = static_cast<const uint16_t*>(x);
-  p.ld = ld; p.rows = rows; p.cols = cols;
-  p.vec_ok = bf16_vec_ok(x, ld);
-  p.bias = rule == FQ_MX_COVER ? 63 : 0;
-  p.stochastic = stochastic; p.seed = seed;
-  p.r = mx_rows(out); p.t = mx_cols(out);
-  return fq::launch_mx_quantize(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+  p->x = static_cast<const uint16_t*>(x);
+  p->ld = ld; p->rows = rows; p->cols = cols;
+  p->bias = rule == FQ_MX_COVER ? 63 : 0;
+  p->r = mx_rows(out); p->t = mx_cols(out);
+  return FQ_OK;
 }
 
 // Validates a product and fills its parameters; an empty output is valid (M or N 0).
@@ -540,7 +539,6 @@ fq_status prepare_mx_gemm(fq_op op, const fq_mx_tensor* A, const fq_mx_tensor* B
   if (g->M == 0 || g->N == 0) return FQ_OK;
   if (!C) return FQ_ERR_NULL;
   g->c = C; g->ldc = ldc; g->out_bf16 = cdt == FQ_OUT_BF16;
-  g->vec_ok = ((uintptr_t)C & 15) == 0 && ldc * (g->out_bf16 ? 2 : 4) % 16 == 0;
   return FQ_OK;
 }
 }  // namespace
@@ -573,12 +571,19 @@ fq_status fq_mx_bind(void* base, int32_t rows, int32_t cols, int32_t sides, fq_m
 
 fq_status fq_mx_quantize(const void* x_bf16, int32_t rows, int32_t cols, int64_t ld, fq_mx_rule rule, fq_mx_tensor* out,
                          void* hip_stream) {
-  return mx_quantize_impl(x_bf16, rows, cols, ld, rule, false, 0, out, hip_stream);
+  fq::MxQuantParams p;
+  const fq_status s = prepare_mx_quantize(x_bf16, rows, cols, ld, rule, out, &p);
+  if (s != FQ_OK || !p.x) return s;
+  return fq::launch_mx_quantize(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
 fq_status fq_mx_quantize_sr(const void* x_bf16, int32_t rows, int32_t cols, int64_t ld, uint64_t seed, fq_mx_tensor* out,
                             void* hip_stream) {
-  return mx_quantize_impl(x_bf16, rows, cols, ld, FQ_MX_COVER, true, seed, out, hip_stream);
+  fq::MxQuantParams p;
+  const fq_status s = prepare_mx_quantize(x_bf16, rows, cols, ld, FQ_MX_COVER, out, &p);
+  if (s != FQ_OK || !p.x) return s;
+  p.stochastic = 1; p.seed = seed;
+  return fq::launch_mx_quantize(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
 fq_status fq_mx_dequantize(const fq_mx_tensor* t, int32_t side, void* out, fq_out_dtype odt, int64_t ldo, void* hip_stream) {
@@ -594,7 +599,6 @@ fq_status fq_mx_dequantize(const fq_mx_tensor* t, int32_t side, void* out, fq_ou
   if (!out) return FQ_ERR_NULL;
   p.columns = side == FQ_MX_COLS;
   p.out = out; p.ldo = ldo; p.rows = t->rows; p.cols = t->cols; p.out_bf16 = odt == FQ_OUT_BF16;
-  p.vec_ok = ((uintptr_t)out & 15) == 0 && ldo * (p.out_bf16 ? 2 : 4) % 16 == 0;
   return fq::launch_mx_dequantize(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
@@ -606,18 +610,51 @@ fq_status fq_mx_gemm(fq_op op, const fq_mx_tensor* A, const fq_mx_tensor* B, voi
   return fq::launch_mx_gemm(g, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
+static_assert((int)fq::MxForm::k32x32 == FQ_MX_FORM_32x32 && (int)fq::MxForm::k32x64 == FQ_MX_FORM_32x64 &&
+              (int)fq::MxForm::k64x64 == FQ_MX_FORM_64x64 && (int)fq::MxForm::k128x128 == FQ_MX_FORM_128x128 &&
+              (int)fq::MxForm::k256x256 == FQ_MX_FORM_256x256);
+
+fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contraction, int32_t compute_units, int32_t form[2]) {
+  if (!form) return FQ_ERR_NULL;
+  if (rows_out < 0 || cols_out < 0 || contraction < 0) return FQ_ERR_SHAPE;
+  const int cus = compute_units > 0 ? compute_units : fq::planning_cus();
+  if (cus <= 0) return FQ_ERR_HIP;
+  form[0] = rows_out && cols_out ? (int32_t)fq::mx_form(rows_out, cols_out, (int)ceil_div(contraction, 128), cus) : 0;
+  form[1] = rows_out && cols_out ? fq::mx_linear_fused(rows_out, cols_out, contraction, cus) : 0;
+  return FQ_OK;
+}
+
 fq_status fq_mx_linear(const void* x_bf16, int32_t rows, int64_t ld, fq_mx_rule rule, const fq_mx_tensor* W,
                        fq_mx_tensor* xq, void* Y, fq_out_dtype ydt, int64_t ldy, void* hip_stream) {
   // everything is checked before the first launch
-  if (!W || !xq) return FQ_ERR_NULL;
+  if (!W) return FQ_ERR_NULL;
+  fq_mx_tensor side{rows, W->cols, nullptr, nullptr, nullptr, nullptr};      // X's rows' side
+  if (xq) {
+    const fq_status s = check_mx(xq);
+    if (s != FQ_OK) return s;
+    if (xq->rows != rows || xq->cols != W->cols) return FQ_ERR_SHAPE;
+    side.codes = xq->codes;
+    side.scales = xq->scales;
+  } else if (rows > FQ_MX_LINEAR_ROWS) {
+    return FQ_ERR_NULL;
+  } else {
+    side.codes = side.scales = reinterpret_cast<uint8_t*>(16);      // not written
+  }
   fq::MxGemmParams g;
-  fq_status s = prepare_mx_gemm(FQ_OP_NT, xq, W, Y, ydt, ldy, &g);
+  fq_status s = prepare_mx_gemm(FQ_OP_NT, &side, W, Y, ydt, ldy, &g);
   if (s != FQ_OK) return s;
-  fq_mx_tensor side = *xq;       // only the rows' side is needed
-  side.codes_t = side.scales_t = nullptr;
-  s = mx_quantize_impl(x_bf16, rows, W->cols, ld, rule, false, 0, &side, hip_stream);
+  fq::MxQuantParams q;
+  s = prepare_mx_quantize(x_bf16, rows, W->cols, ld, rule, &side, &q);
   if (s != FQ_OK || g.M == 0 || g.N == 0) return s;
-  return fq::launch_mx_gemm(g, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const int cus = fq::planning_cus();
+  if (cus <= 0) return FQ_ERR_HIP;
+  if (q.x && (!xq || fq::mx_linear_fused(g.M, g.N, q.cols, cus))) {
+    g.x = q.x; g.ld = q.ld; g.K = q.cols; g.bias = q.bias;
+  } else if (q.x && fq::launch_mx_quantize(q, st) != hipSuccess) {
+    return FQ_ERR_HIP;
+  }
+  return fq::launch_mx_gemm(g, st) == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
 fq_status fq_gemm_tile_plan(int32_t rows_out, int32_t cols_out, int32_t compute_units,

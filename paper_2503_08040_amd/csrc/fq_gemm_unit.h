@@ -176,6 +176,16 @@ __device__ __forceinline__ void load_lds_dword(const void* from, unsigned off, u
   asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %0\n\tglobal_load_lds_dword %2, %0"
                : "+s"(base) : "s"(to), "v"(off) : "memory", "m0");
 }
+// 16 bytes per lane from base + off to dst + 16 lane.
+__device__ __forceinline__ void load_lds_at(const void* from, unsigned off, uint32_t dst) {
+  const uint64_t addr = reinterpret_cast<uint64_t>(from);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)addr);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(addr >> 32));
+  uint64_t base = ((uint64_t)hi << 32) | lo;
+  const uint32_t to = __builtin_amdgcn_readfirstlane(dst);
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %0\n\tglobal_load_lds_dwordx4 %2, %0"
+               : "+s"(base) : "s"(to), "v"(off) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 }  // namespace

@@ -142,7 +142,6 @@ struct MxQuantParams {
   const uint16_t* x;   // bf16 bits, row-major [rows, ld]
   int64_t ld;
   int rows, cols;
-  int vec_ok;          // 16-byte loads
   int bias;            // added to a group's largest bf16 magnitude before its exponent is taken: 0 FLOOR, 63 COVER
   int stochastic;
   uint64_t seed;
@@ -155,7 +154,6 @@ struct MxDequantParams {
   void* out;           // row-major [rows, ldo]
   int64_t ldo;
   int rows, cols;
-  int vec_ok;          // 16-byte stores
   int out_bf16;
 };
 
@@ -165,12 +163,21 @@ struct MxGemmParams {
   int64_t ldc;
   int M, N;
   int out_bf16;
-  int vec_ok;          // C's base and pitch allow 16-byte stores
+  // A in bf16, quantized on the way: a has sizes only
+  const uint16_t* x;   // [M, ld]; nullptr: A is stored
+  int64_t ld;
+  int K;
+  int bias;            // as in MxQuantParams
 };
 
 hipError_t launch_mx_quantize(const MxQuantParams& p, hipStream_t st);
 hipError_t launch_mx_dequantize(const MxDequantParams& p, hipStream_t st);
 hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st);
+// the tiles of an M x N output over nkb blocks of 128 on that many compute units
+enum class MxForm { k32x32, k32x64, k64x64, k128x128, k256x256 };
+MxForm mx_form(int M, int N, int nkb, int cus);
+// whether a linear layer's forward quantizes X inside its product
+bool mx_linear_fused(int M, int N, int K, int cus);
 
 hipError_t launch_quantize(const QuantParams& p, hipStream_t st);
 hipError_t launch_untile(const int8_t* tiled, int rows, int cols, int8_t* dense, hipStream_t st);
@@ -192,6 +199,8 @@ void gemm_tile_plan(int nib, int njb, int cus, int out[3]);
 void gemm_path(int M, int N, int cus, bool biased, int out[4]);
 // out = {SmallTile, workgroups}: what launch_gemm launches for an A with or without residual slots.
 void gemm_form(int M, int N, int K, int cus, bool biased, bool slots, int out[2]);
+// the current device's compute units (or FQ_GEMM_CUS); -1 if they cannot be had
+int planning_cus();
 hipError_t launch_rmsnorm(const RmsParams& p, bool backward, hipStream_t st);
 hipError_t launch_glu(const GluParams& p, bool backward, hipStream_t st);
 hipError_t launch_ctx(const CtxParams& p, bool dequantize, hipStream_t st);

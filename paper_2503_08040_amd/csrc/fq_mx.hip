@@ -11,6 +11,7 @@
 // to leave in 16-byte stores.
 #include "fq_device.h"
 #include "fq_kernels.h"
+#include "fq_mx_device.h"
 
 namespace fq {
 
@@ -19,56 +20,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTile = 128;        // rows and columns of a workgroup: whole operands along either axis
 constexpr int kWaveRows = 32;     // of a wavefront: one group along the columns
-constexpr int kOperand = 1024;    // 16 rows x 128
-constexpr int kScaleBlock = 256;  // scales of 64 rows x 128
-
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef uint16_t v2h __attribute__((ext_vector_type(2)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2h, a), __builtin_bit_cast(v2h, b)));
-}
-
-// maximum over the 4 lanes of a quad
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-  v = pk_max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lanes 1, 0, 3, 2
-  return pk_max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // lanes 2, 3, 0, 1
-}
-
-// maximum over the 4 lanes 16 apart
-__device__ __forceinline__ uint32_t row_max(uint32_t v) {
-  v2u s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  v = pk_max(s[0], s[1]);
-  s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  return pk_max(s[0], s[1]);
-}
-
-// Scale byte of a group with largest magnitude m (bf16 bits without the sign).  bias 63 takes the next exponent if
-// the mantissa is above 1.5; the smallest byte is 0.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t m, int bias) {
-  const uint32_t e = (m + (uint32_t)bias) >> 7;
-  return m >= 0x7F80u ? 255u : (e > 2u ? e : 2u) - 2u;
-}
-
-// 2^(byte - 127) as the conversions take it; 2^-127 is a subnormal number.
-__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
-
-// 2^(127 - byte): multiplication by it divides by the scale.
-__device__ __forceinline__ float scale_inverse(uint32_t byte) {
-  return __uint_as_float(byte < 254u ? (254u - byte) << 23 : 0x00400000u);
-}
-
-__device__ __forceinline__ uint32_t cvt_fp4(uint32_t old, uint32_t pair, float scale, int sel) {
-  const v2bf v = __builtin_bit_cast(v2bf, pair);
-  switch (sel) {
-    case 0: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 0);
-    case 1: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 1);
-    case 2: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 2);
-    default: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, v, scale, 3);
-  }
-}
 
 // Stochastic code of a bf16 value (bits) with 16 random bits: t = |x| / 2^s in units of 2^-17, the step above it is
 // 2^16, 2^17 or 2^18 of them; the sum of t and the random part of a step is cut to whole steps.  A finite group has
@@ -100,8 +51,8 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
     x[i] = v4u{0u, 0u, 0u, 0u};
     if (row < p.rows && col0 < p.cols) {
       const uint16_t* src = p.x + row * p.ld + col0;
-      if (p.vec_ok && col0 + 8 <= p.cols) {
-        x[i] = *reinterpret_cast<const v4u*>(src);
+      if (col0 + 8 <= p.cols) {
+        x[i] = *reinterpret_cast<const v4u_at2*>(src);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -270,11 +221,11 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxDequantParams
   for (int i = 0; i < 8; ++i) {
     if (row0 + i >= p.rows) break;
     const int64_t o = (row0 + i) * p.ldo + col0;
-    const bool whole = p.vec_ok && col0 + 8 <= p.cols;
+    const bool whole = col0 + 8 <= p.cols;
     if constexpr (kBf16) {
       uint16_t* dst = static_cast<uint16_t*>(p.out) + o;
       if (whole) {
-        *reinterpret_cast<v4u*>(dst) = v4u{y[i][0], y[i][1], y[i][2], y[i][3]};
+        *reinterpret_cast<v4u_at2*>(dst) = v4u{y[i][0], y[i][1], y[i][2], y[i][3]};
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -285,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxDequantParams
       if (whole) {
 #pragma unroll
         for (int d = 0; d < 2; ++d)
-          reinterpret_cast<v4u*>(dst)[d] = v4u{y[i][2 * d] << 16, y[i][2 * d] & 0xFFFF0000u, y[i][2 * d + 1] << 16,
+          *reinterpret_cast<v4u_at2*>(dst + 4 * d) = v4u{y[i][2 * d] << 16, y[i][2 * d] & 0xFFFF0000u, y[i][2 * d + 1] << 16,
                                                y[i][2 * d + 1] & 0xFFFF0000u};
       } else {
 #pragma unroll

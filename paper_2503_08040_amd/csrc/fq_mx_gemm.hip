@@ -4,10 +4,14 @@
 // and the byte of their scale, and adds the exact products in binary32.  So a product here is a plain matrix loop on
 // 17/32 byte an element.  The storage order (fq.h) makes 1 KiB of codes one operand, lane by lane, and a dword of
 // scales the four operands of 64 rows, told apart by the instruction's byte select.
+#include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "fq_device.h"
+#include "fq_gemm_unit.h"
 #include "fq_kernels.h"
+#include "fq_mx_device.h"
 
 namespace fq {
 
@@ -16,11 +20,9 @@ namespace {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v2f __attribute__((ext_vector_type(2)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
-constexpr int kOperand = 1024;    // 16 rows x 128
-constexpr int kScaleBlock = 256;  // scales of 64 rows x 128
+constexpr int kMaxDevices = 64;   // per-device host-side caches
+constexpr int kMaxBlocks = 1 << 22;   // blocks of a contraction whose codes' offsets fit 32 bits
 constexpr int kFp4 = 4;           // the instruction's format code of E2M1
 
 // acc += a b with byte kSa of sa, kSb of sb: rows of `a` go to registers, rows of `b` to lanes, so with C's columns
@@ -41,18 +43,22 @@ __device__ __forceinline__ v4f mfma_select(const v4i& a, const v4i& b, const v4f
   }
 }
 
+__device__ __forceinline__ v2u pack_bf16(const v4f& v) {
+  const v2f lo = {v[0], v[1]}, hi = {v[2], v[3]};
+  return v2u{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, v2bf)),
+             __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, v2bf))};
+}
+
 // 4 consecutive values of a row of C
 __device__ __forceinline__ void store4(const MxGemmParams& p, const v4f& v, int row, int col) {
   if (row >= p.M || col >= p.N) return;
   const int64_t o = (int64_t)row * p.ldc + col;
-  const bool whole = p.vec_ok && col + 4 <= p.N;
+  const bool whole = col + 4 <= p.N;
   if (p.out_bf16) {
     uint16_t* dst = static_cast<uint16_t*>(p.c) + o;
-    const v2f lo = {v[0], v[1]}, hi = {v[2], v[3]};
-    const v2u b = {__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, v2bf)),
-                   __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, v2bf))};
+    const v2u b = pack_bf16(v);
     if (whole) {
-      *reinterpret_cast<v2u*>(dst) = b;
+      *reinterpret_cast<v2u_at2*>(dst) = b;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -61,7 +67,7 @@ __device__ __forceinline__ void store4(const MxGemmParams& p, const v4f& v, int 
   } else {
     float* dst = static_cast<float*>(p.c) + o;
     if (whole) {
-      *reinterpret_cast<v4f*>(dst) = v;
+      *reinterpret_cast<v4f_at4*>(dst) = v;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -70,24 +76,58 @@ __device__ __forceinline__ void store4(const MxGemmParams& p, const v4f& v, int 
   }
 }
 
+// 32 values of a bf16 row, from column `col` on, as packed pairs; what is not there reads as 0.
+__device__ __forceinline__ void load_group(const MxGemmParams& p, int row, int col, v4u (&x)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = v4u{0u, 0u, 0u, 0u};
+  if (row >= p.M) return;
+  const uint16_t* const src = p.x + row * p.ld + col;
+  if (col + 32 <= p.K) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const v4u_at2*>(src + 8 * i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (col + i < p.K) x[i >> 3][(i >> 1) & 3] |= (uint32_t)src[i] << (16 * (i & 1));
+  }
+}
+
+// Codes and scale byte of a group, the same as mx_quantize_kernel's.
+__device__ __forceinline__ uint32_t quantize_group(const v4u (&x)[4], int bias, v4i& codes) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = pk_max(m, x[i >> 2][i & 3] & 0x7FFF7FFFu);
+  const uint32_t byte = scale_byte(max(m >> 16, m & 0xFFFFu), bias);
+  const float s = scale_value(byte);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t c = 0;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) c = cvt_fp4(c, x[i][d], s, d);
+    codes[i] = byte == 255u ? 0 : (int)c;
+  }
+  return byte;
+}
+
 // ---- small outputs: a workgroup per tile of kM x kN strips, the contraction split over its kW wavefronts -----------
 // Operands go straight from memory to registers, kU blocks of 128 at a time; the wavefronts' sums are joined through
-// LDS in a fixed order.
-template <int kM, int kN, int kW, int kU>
+// LDS in a fixed order.  kFused: A is bf16 and every workgroup quantizes the rows of its tile as it goes.
+template <int kM, int kN, int kW, int kU, bool kFused>
 __global__ __launch_bounds__(64 * kW) void mx_gemm_split_kernel(MxGemmParams p, int tiles_j) {
   static_assert(4 % kM == 0 && 4 % kN == 0, "the strips of a tile share their scale dwords");
   __shared__ v4f part[kW][kM * kN][64];
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ti = blockIdx.x / tiles_j, tj = blockIdx.x % tiles_j;
-  const int i0 = ti * kM, j0 = tj * kN, nkb = p.a.nkb;
+  const int i0 = ti * kM, j0 = tj * kN, nkb = p.b.nkb;
   // strips behind the last one repeat it: their results are not stored
   const uint8_t *ap[kM], *bp[kN];
 #pragma unroll
-  for (int i = 0; i < kM; ++i) ap[i] = p.a.codes + (int64_t)min(i0 + i, p.a.strips - 1) * nkb * kOperand + lane * 16;
+  for (int i = 0; i < kM; ++i)
+    ap[i] = kFused ? nullptr : p.a.codes + (int64_t)min(i0 + i, p.a.strips - 1) * nkb * kOperand + lane * 16;
 #pragma unroll
   for (int j = 0; j < kN; ++j) bp[j] = p.b.codes + (int64_t)min(j0 + j, p.b.strips - 1) * nkb * kOperand + lane * 16;
-  const uint8_t* const as = p.a.scales + (int64_t)(i0 >> 2) * nkb * kScaleBlock + lane * 4;
+  const uint8_t* const as = kFused ? nullptr : p.a.scales + (int64_t)(i0 >> 2) * nkb * kScaleBlock + lane * 4;
   const uint8_t* const bs = p.b.scales + (int64_t)(j0 >> 2) * nkb * kScaleBlock + lane * 4;
   const int ash = 8 * (i0 & 3), bsh = 8 * (j0 & 3);
   v4f acc[kM][kN];
@@ -96,30 +136,55 @@ __global__ __launch_bounds__(64 * kW) void mx_gemm_split_kernel(MxGemmParams p, 
 #pragma unroll
     for (int j = 0; j < kN; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
-  auto blocks = [&](int kb, auto n_c) {
-    constexpr int n = decltype(n_c)::value;
-    v4i a[n][kM], b[n][kN];
-    uint32_t sa[n], sb[n];
+  // kU blocks' operands are requested while those of the kU before are multiplied
+  struct Set {
+    v4i a[kU][kM], b[kU][kN];
+    v4u x[kU][kM][4];
+    uint32_t sa[kU], sb[kU];
+  };
+  auto request = [&](Set& s, int kb) {
 #pragma unroll
-    for (int u = 0; u < n; ++u) {
-      const int64_t k = kb + u * kW;
+    for (int u = 0; u < kU; ++u) {
+      const int k = kb + u * kW;
+      if (k >= nkb) break;
 #pragma unroll
-      for (int i = 0; i < kM; ++i) a[u][i] = *reinterpret_cast<const v4i*>(ap[i] + k * kOperand);
+      for (int j = 0; j < kN; ++j) s.b[u][j] = *reinterpret_cast<const v4i*>(bp[j] + (int64_t)k * kOperand);
+      s.sb[u] = *reinterpret_cast<const uint32_t*>(bs + (int64_t)k * kScaleBlock) >> bsh;
+      if constexpr (kFused) {
 #pragma unroll
-      for (int j = 0; j < kN; ++j) b[u][j] = *reinterpret_cast<const v4i*>(bp[j] + k * kOperand);
-      sa[u] = *reinterpret_cast<const uint32_t*>(as + k * kScaleBlock) >> ash;
-      sb[u] = *reinterpret_cast<const uint32_t*>(bs + k * kScaleBlock) >> bsh;
+        for (int i = 0; i < kM; ++i)
+          load_group(p, (i0 + i) * 16 + (lane & 15), k * 128 + 32 * (lane >> 4), s.x[u][i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kM; ++i) s.a[u][i] = *reinterpret_cast<const v4i*>(ap[i] + (int64_t)k * kOperand);
+        s.sa[u] = *reinterpret_cast<const uint32_t*>(as + (int64_t)k * kScaleBlock) >> ash;
+      }
     }
+  };
+  auto multiply = [&](Set& s, int kb) {
 #pragma unroll
-    for (int u = 0; u < n; ++u)
+    for (int u = 0; u < kU; ++u) {
+      if (kb + u * kW >= nkb) break;
+      if constexpr (kFused) {
+        s.sa[u] = 0;
+#pragma unroll
+        for (int i = 0; i < kM; ++i) s.sa[u] |= quantize_group(s.x[u][i], p.bias, s.a[u][i]) << (8 * i);
+      }
 #pragma unroll
       for (int i = 0; i < kM; ++i)
 #pragma unroll
-        for (int j = 0; j < kN; ++j) acc[i][j] = mfma_select(b[u][j], a[u][i], acc[i][j], j, (int)sb[u], i, (int)sa[u]);
+        for (int j = 0; j < kN; ++j)
+          acc[i][j] = mfma_select(s.b[u][j], s.a[u][i], acc[i][j], j, (int)s.sb[u], i, (int)s.sa[u]);
+    }
   };
-  int kb = w;
-  for (; kb + (kU - 1) * kW < nkb; kb += kU * kW) blocks(kb, std::integral_constant<int, kU>{});
-  for (; kb < nkb; kb += kW) blocks(kb, std::integral_constant<int, 1>{});
+  Set even, odd;
+  request(even, w);
+  for (int kb = w; kb < nkb; kb += 2 * kU * kW) {
+    request(odd, kb + kU * kW);
+    multiply(even, kb);
+    request(even, kb + 2 * kU * kW);
+    multiply(odd, kb + kU * kW);
+  }
 
 #pragma unroll
   for (int i = 0; i < kM; ++i)
@@ -134,17 +199,329 @@ __global__ __launch_bounds__(64 * kW) void mx_gemm_split_kernel(MxGemmParams p, 
   }
 }
 
-template <int kM, int kN, int kW, int kU>
-void split(const MxGemmParams& p, hipStream_t st) {
+// The same instruction in place and in order.  With 256 of 512 registers as accumulators the compiler's allocation of its
+// own form moves them about in the loop.  What follows a matrix instruction and reads acc other than as another's
+// accumulator has to wait by itself.
+template <int kSa, int kSb>
+__device__ __forceinline__ void mfma_in_place(v4f& acc, const v4i& a, const v4i& b, int sa, int sb) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0] cbsz:4 blgp:4"
+               : "+a"(acc) : "v"(a), "v"(b), "v"(sa), "v"(sb), "n"(kSa & 1), "n"(kSb & 1), "n"(kSa >> 1), "n"(kSb >> 1));
+}
+
+__device__ __forceinline__ void mfma_in_place_select(v4f& acc, const v4i& a, const v4i& b, int ia, int sa, int ib, int sb) {
+  switch (4 * (ia & 3) + (ib & 3)) {
+#define FQ_CASE(x, y) case 4 * x + y: return mfma_in_place<x, y>(acc, a, b, sa, sb);
+    FQ_CASE(0, 0) FQ_CASE(0, 1) FQ_CASE(0, 2) FQ_CASE(0, 3) FQ_CASE(1, 0) FQ_CASE(1, 1) FQ_CASE(1, 2) FQ_CASE(1, 3)
+    FQ_CASE(2, 0) FQ_CASE(2, 1) FQ_CASE(2, 2) FQ_CASE(2, 3) FQ_CASE(3, 0) FQ_CASE(3, 1) FQ_CASE(3, 2)
+    default: return mfma_in_place<3, 3>(acc, a, b, sa, sb);
+#undef FQ_CASE
+  }
+}
+
+// ---- large outputs: 2 x kWC wavefronts of 16 kR x 16 kC, operands through LDS ----------------------------------------
+// A stage is one block of 128 of the contraction: codes of the tile's strips, then their scales, brought by direct
+// global -> LDS loads.  There are kStages of them: while a block is multiplied out of registers, the next one's operands
+// are fetched from LDS and up to three more blocks are under way.  A workgroup walks over several tiles and the ring of
+// stages runs on from one to the next, so that only the first tile waits for its operands.
+template <int kR_, int kC_, int kWC_, int kOcc_>
+struct LdsGeo {
+  static constexpr int kR = kR_, kC = kC_, kWC = kWC_, kOcc = kOcc_;        // strips of a wavefront; workgroups of a CU
+  static constexpr int kWaves = 2 * kWC, kThreads = 64 * kWaves;
+  static constexpr int kStages = 4;
+  static constexpr int kStrips = 2 * kR;                                    // of the tile along either axis
+  static constexpr int kLoads = kStrips * 2 / kWaves;                       // strips that a wavefront loads
+  static constexpr int kQuads = kStrips / 4, kScaleLoads = kQuads * 2 / kWaves;   // 64 rows' scales along an axis; loads of them
+  static constexpr int kCodes = kStrips * 2 * kOperand;                     // bytes of a stage
+  static constexpr int kStage = kCodes + kQuads * 2 * kScaleBlock;
+  static constexpr int kPatchRow = 128, kPatch = 16 * kPatchRow;            // a wavefront's patch for C
+  static constexpr int kLds = kStages * kStage + kWaves * kPatch;
+  static_assert(kR % 4 == 0 && kC % 4 == 0 && kC * kWC == kStrips && kOcc * kLds <= 160 * 1024);
+  static_assert(kLoads * kWaves == 2 * kStrips && kScaleLoads * kWaves == 2 * kQuads && kLoads == 4 * kScaleLoads);
+};
+
+// 16 rows of kChunks 16-byte chunks from a patch in LDS to C at (row0, col0); chunk c of row r lies at c ^ r.
+template <int kChunks, class T>
+__device__ __forceinline__ void store_patch(const MxGemmParams& p, const int8_t* patch, int row0, int col0, int lane) {
+  constexpr int kPer = 16 / (int)sizeof(T), kStep = 64 / kChunks;      // elements of a chunk, rows of a store
+  const int c = lane % kChunks, col = col0 + c * kPer, r0 = lane / kChunks;
+  T* const dst = static_cast<T*>(p.c) + (int64_t)(row0 + r0) * p.ldc + col;
+  auto from = [&](int i) { return patch + (r0 + i * kStep) * kChunks * 16 + ((c ^ (r0 + i * kStep)) & (kChunks - 1)) * 16; };
+  if (row0 + 16 <= p.M && col0 + kChunks * kPer <= p.N) {
+#pragma unroll
+    for (int i = 0; i < 16 / kStep; ++i)
+      *reinterpret_cast<v4u_at2*>(dst + i * kStep * p.ldc) = *reinterpret_cast<const v4u*>(from(i));
+  } else {
+    const int valid = min(p.N - col, kPer);
+#pragma unroll 1
+    for (int i = 0; i < 16 / kStep; ++i) {
+      if (row0 + r0 + i * kStep >= p.M) break;
+      const T* const v = reinterpret_cast<const T*>(from(i));
+      if (valid == kPer) {
+        *reinterpret_cast<v4u_at2*>(dst + i * kStep * p.ldc) = *reinterpret_cast<const v4u*>(v);
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < valid; ++e) dst[i * kStep * p.ldc + e] = v[e];
+      }
+    }
+  }
+}
+
+template <class G, class T>
+__global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_lds_kernel(MxGemmParams p, int tiles_i, int tiles_j) {
+  extern __shared__ __attribute__((aligned(1024))) int8_t lds[];
+  constexpr int kR = G::kR, kC = G::kC, kLoads = G::kLoads, kScaleLoads = G::kScaleLoads;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = w / G::kWC, wc = w % G::kWC;
+  const int nkb = p.a.nkb, tiles = tiles_i * tiles_j;
+  const uint32_t lds0 = lds_address(lds);
+  auto tile_of = [&](int b, int& i0, int& j0) {      // first strips of this workgroup's b-th tile
+    int ti, tj;
+    tile_at<4>(xcd_run(b, tiles), tiles_i, tiles_j, ti, tj);
+    i0 = ti * G::kStrips;
+    j0 = tj * G::kStrips;
+  };
+
+  // The loader's side.  What this wavefront loads of a tile: kLoads strips, the first half of the wavefronts of A, the
+  // others of B, and kScaleLoads times 64 rows' scales; behind the end the last ones again.
+  const bool of_b = w >= G::kWaves / 2;
+  const MxSide side = of_b ? p.b : p.a;
+  const int8_t *strip[kLoads], *quad[kScaleLoads];
+  auto aim = [&](int b) {
+    int i0, j0;
+    tile_of(b, i0, j0);
+    const int s0 = (of_b ? j0 : i0) + w % (G::kWaves / 2) * kLoads;
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n)
+      strip[n] = reinterpret_cast<const int8_t*>(side.codes) + (int64_t)min(s0 + n, side.strips - 1) * nkb * kOperand;
+#pragma unroll
+    for (int n = 0; n < kScaleLoads; ++n)
+      quad[n] = reinterpret_cast<const int8_t*>(side.scales) + (int64_t)min((s0 >> 2) + n, side.quads - 1) * nkb * kScaleBlock;
+  };
+  int aimed = blockIdx.x, ahead = 0;      // tile and block to load next
+  unsigned code_off = lane * 16u, scale_off = lane * 4u;
+  uint32_t stage_at = lds0;
+  aim(aimed);
+  auto load = [&](int n) {
+    if (n < kLoads) load_lds_at(strip[n], code_off, stage_at + (w * kLoads + n) * kOperand);
+    else load_lds_dword(quad[n - kLoads], scale_off, stage_at + G::kCodes + (w * kScaleLoads + n - kLoads) * kScaleBlock);
+  };
+  constexpr int kAllLoads = kLoads + kScaleLoads;
+  // the block behind: of the next tile, or behind the last tile the last block again, into a stage that nobody reads
+  auto advance = [&]() {
+    stage_at = stage_at == lds0 + (G::kStages - 1) * G::kStage ? lds0 : stage_at + G::kStage;
+    code_off += kOperand;
+    scale_off += kScaleBlock;
+    if (++ahead < nkb) return;
+    if (aimed + (int)gridDim.x < tiles) {
+      aimed += gridDim.x;
+      aim(aimed);
+      code_off -= (unsigned)nkb * kOperand;
+      scale_off -= (unsigned)nkb * kScaleBlock;
+      ahead = 0;
+    } else {
+      --ahead;
+      code_off -= kOperand;
+      scale_off -= kScaleBlock;
+    }
+  };
+  // until at most n stages are under way; lgkmcnt(0)
+  auto wait_stages = [](auto n_c) {
+    constexpr int n = decltype(n_c)::value * kAllLoads;
+    static_assert(n < 64);
+    __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 0x0070);
+  };
+
+  // The multiplier's side.
+  v4f acc[kR][kC];
+  struct Operands {
+    v4i a[kR], b[kC];
+    int sa[kR / 4], sb[kC / 4];
+  } f[2];
+  const int aoff = wr * kR * kOperand + lane * 16, boff = (G::kStrips + wc * kC) * kOperand + lane * 16;
+  const int saoff = G::kCodes + wr * (kR / 4) * kScaleBlock + lane * 4;
+  const int sboff = G::kCodes + (G::kQuads + wc * (kC / 4)) * kScaleBlock + lane * 4;
+  const int8_t* rd = lds;      // stage of the operands to fetch
+  // a block's fetches and a stage's loads, spread over the products of a block
+  constexpr int kFetch = kR + kC + kR / 4 + kC / 4, kFetchStep = kR * kC >= 2 * kFetch ? 2 : 1, kLoadStep = kR * kC / kAllLoads;
+  static_assert(kFetch * kFetchStep <= kR * kC && kLoadStep > 0);
+  auto fetch = [&](Operands& o, int n) {
+    if (n < kC) o.b[n] = *reinterpret_cast<const v4i*>(rd + boff + n * kOperand);
+    else if (n < kC + kR) o.a[n - kC] = *reinterpret_cast<const v4i*>(rd + aoff + (n - kC) * kOperand);
+    else if (n < kC + kR + kC / 4) o.sb[n - kC - kR] = *reinterpret_cast<const int*>(rd + sboff + (n - kC - kR) * kScaleBlock);
+    else if (n < kFetch)
+      o.sa[n - kC - kR - kC / 4] = *reinterpret_cast<const int*>(rd + saoff + (n - kC - kR - kC / 4) * kScaleBlock);
+  };
+  auto next_stage = [&]() { rd = rd == lds + (G::kStages - 1) * G::kStage ? lds : rd + G::kStage; };
+  // a block out of `o`, the next one into `other`
+  auto block = [&](const Operands& o, Operands& other) {
+    // the next block is there, and everybody has this one's operands in registers, so its stage is free
+    wait_stages(std::integral_constant<int, 2>{});
+    asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+      for (int j = 0; j < kC; ++j) {
+        mfma_in_place_select(acc[i][j], o.b[j], o.a[i], j, o.sb[j >> 2], i, o.sa[i >> 2]);
+        const int n = i * kC + j;
+        if (n % kFetchStep == 0) fetch(other, n / kFetchStep);
+        if (n % kLoadStep == 0 && n / kLoadStep < kAllLoads) load(n / kLoadStep);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    advance();
+    next_stage();
+  };
+
+#pragma unroll 1
+  for (int k = 0; k < G::kStages; ++k) {
+#pragma unroll
+    for (int n = 0; n < kAllLoads; ++n) load(n);
+    advance();
+  }
+  wait_stages(std::integral_constant<int, G::kStages - 1>{});
+  asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+  for (int n = 0; n < kFetch; ++n) fetch(f[0], n);
+  next_stage();
+
+#pragma unroll 1
+  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+      for (int j = 0; j < kC; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    int left = nkb;
+#pragma unroll 1
+    for (; left > 1; left -= 2) {
+      block(f[0], f[1]);
+      block(f[1], f[0]);
+    }
+    if (left) {
+      block(f[0], f[1]);
+      const Operands o = f[0];
+      f[0] = f[1];
+      f[1] = o;
+    }
+    // 32 wait states for the last products, more than any matrix instruction of 4 passes needs before its result is read
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    int i0, j0;
+    tile_of(t, i0, j0);
+    // C leaves strip by strip through a patch of the wavefront's own, so that rows are stored in pieces of kPatchRow bytes.
+    constexpr int kChunks = G::kPatchRow / 16, kPass = G::kPatchRow / (16 * (int)sizeof(T));
+    int8_t* const patch = lds + G::kStages * G::kStage + w * G::kPatch;
+    const int r = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+      for (int jj = 0; jj < kC; jj += kPass) {
+#pragma unroll
+        for (int j = 0; j < kPass; ++j) {
+          asm volatile("" : "+a"(acc[i][jj + j]));      // read here and not before
+          const int at = (16 * j + 4 * q) * (int)sizeof(T);
+          int8_t* const dst = patch + r * G::kPatchRow + (((at >> 4) ^ r) & (kChunks - 1)) * 16 + (at & 15);
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<v2u*>(dst) = pack_bf16(acc[i][jj + j]);
+          else *reinterpret_cast<v4f*>(dst) = acc[i][jj + j];
+        }
+        store_patch<kChunks, T>(p, patch, (i0 + wr * kR + i) * 16, (j0 + wc * kC + jj) * 16, lane);
+      }
+  }
+  wait_stages(std::integral_constant<int, 0>{});      // nothing may be under way into LDS when the workgroup ends
+}
+
+template <class G, class T>
+hipError_t through_lds(const MxGemmParams& p, int cus, hipStream_t st) {
+  // the kernel needs more dynamic LDS than the default limit: raise it once per device
+  static std::atomic<bool> attr_set[kMaxDevices];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx_gemm_lds_kernel<G, T>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds);
+    if (e != hipSuccess) return e;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  const int ti = (p.a.strips + G::kStrips - 1) / G::kStrips, tj = (p.b.strips + G::kStrips - 1) / G::kStrips;
+  const int grid = std::min(ti * tj, G::kOcc * cus);
+  hipLaunchKernelGGL((mx_gemm_lds_kernel<G, T>), dim3(grid), dim3(G::kThreads), G::kLds, st, p, ti, tj);
+  return hipGetLastError();
+}
+
+template <class G>
+hipError_t through_lds(const MxGemmParams& p, int cus, hipStream_t st) {
+  return p.out_bf16 ? through_lds<G, uint16_t>(p, cus, st) : through_lds<G, float>(p, cus, st);
+}
+
+template <int kM, int kN, int kW, int kU, bool kFused>
+hipError_t split(const MxGemmParams& p, hipStream_t st) {
   const int ti = (p.a.strips + kM - 1) / kM, tj = (p.b.strips + kN - 1) / kN;
-  hipLaunchKernelGGL((mx_gemm_split_kernel<kM, kN, kW, kU>), dim3(ti * tj), dim3(64 * kW), 0, st, p, tj);
+  hipLaunchKernelGGL((mx_gemm_split_kernel<kM, kN, kW, kU, kFused>), dim3(ti * tj), dim3(64 * kW), 0, st, p, tj);
+  return hipGetLastError();
 }
 
 }  // namespace
 
+namespace {
+
+int64_t tiles_of(int M, int N, int rows, int cols) {
+  return (int64_t)((M + rows - 1) / rows) * ((N + cols - 1) / cols);
+}
+
+// Microseconds that the tiles of 256 x 256 (one workgroup per compute unit) and of 128 x 128 (two) take, fitted to
+// measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 128 to 11008 on 256 compute units; the
+// model is within 15 % of them where the two are close.  A full round of 256 x 256 tiles takes 5 + 0.82 per block of the
+// contraction (power holds the clock down), a part of a round less; of 128 x 128 tiles, a quarter of that output a
+// tile, 2.5 + 0.535 per block, half a round or less 1 + 0.28.
+double time_256(int64_t n, int nkb, int cus) {
+  const int64_t full = n / cus;
+  const double f = (double)(n % cus) / cus;
+  return 5 + full * (5 + 0.82 * nkb) + (f > 0 ? 2 + 3 * f + (0.52 + 0.3 * f * f) * nkb : 0);
+}
+double time_128(int64_t n, int nkb, int cus) {
+  const int64_t full = n / (2 * cus);
+  const double f = (double)(n % (2 * cus)) / (2 * cus);
+  return 4 + full * (2.5 + 0.535 * nkb) + (f > 0.5 ? 2.5 + 0.52 * nkb : f > 0 ? 1 + 0.28 * nkb : 0);
+}
+
+}  // namespace
+
+// The largest tiles of which there are more than half as many as compute units: fewer leave the chip idle, more move
+// more bytes per product.  1024 x 2048 outputs (128 tiles of 128 x 128, 512 of 64 x 64) take the same time either way,
+// 256 x 11008 (172, 688) 12.6 and 17.9 us at a contraction of 4096, 1024 x 1024 (64, 256) 10.5 and 8.1;
+// 256 x 1024 (64 tiles of 64 x 64, 256 of 32 x 32) 7.0 and 4.7.  A tile more than twice as high or wide as the output
+// is for nothing.
+MxForm mx_form(int M, int N, int nkb, int cus) {
+  const int narrow = std::min(M, N);
+  const int64_t n128 = tiles_of(M, N, 128, 128);
+  if (narrow > 64 && 2 * n128 > cus && nkb > 0 && nkb < kMaxBlocks)
+    return narrow > 128 && time_256(tiles_of(M, N, 256, 256), nkb, cus) < time_128(n128, nkb, cus) ? MxForm::k256x256
+                                                                                                   : MxForm::k128x128;
+  if (narrow > 32 && 2 * tiles_of(M, N, 64, 64) > cus) return MxForm::k64x64;
+  if (N > 32 && 2 * tiles_of(M, N, 32, 64) > cus) return MxForm::k32x64;
+  return MxForm::k32x32;
+}
+
+// The forward of a linear layer quantizes X inside its product where that is the faster way.  A workgroup then reads
+// its 16 rows of X in bf16, four times their codes: 1 x 4096 -> 11008 takes 6.7 us instead of 8.9, 128 x 2048 -> 2048
+// 5.5 instead of 7.1, but 16 x 11008 -> 4096 15 instead of 11; even at 128 KiB.  With more than a workgroup per compute
+// unit W comes that many times.  The sums are those of the stored codes' product: 8 wavefronts share a contraction.
+bool mx_linear_fused(int M, int N, int K, int cus) {
+  const MxForm form = mx_form(M, N, (K + 127) / 128, cus);
+  if (form != MxForm::k32x32 && form != MxForm::k32x64) return false;
+  return (int64_t)std::min(M, 16) * K <= 65536 && (M <= 16 || tiles_of(M, N, 16, 64) <= cus + cus / 4);
+}
+
 hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st) {
-  split<4, 4, 4, 2>(p, st);
-  return hipGetLastError();
+  if (p.x) return split<1, 4, 8, 1, true>(p, st);
+  const int cus = planning_cus();
+  if (cus <= 0) return hipErrorInvalidDevice;
+  switch (mx_form(p.M, p.N, p.a.nkb, cus)) {
+    case MxForm::k32x32: return split<2, 2, 8, 2, false>(p, st);
+    case MxForm::k32x64: return split<2, 4, 8, 2, false>(p, st);
+    case MxForm::k64x64: return split<4, 4, 4, 2, false>(p, st);
+    case MxForm::k128x128: return through_lds<LdsGeo<4, 4, 2, 2>>(p, cus, st);
+    case MxForm::k256x256: return through_lds<LdsGeo<8, 4, 4, 1>>(p, cus, st);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace fq

@@ -61,7 +61,8 @@ def pair(op, M, N, K, seed=0):
 
 OPS = {"NT": fq.FQ_OP_NT, "NN": fq.FQ_OP_NN, "TN": fq.FQ_OP_TN}
 SIZES = [(1, 1, 1), (1, 4096, 1024), (5, 33, 31), (16, 16, 128), (17, 65, 129), (33, 200, 700), (64, 64, 2048),
-         (130, 70, 1), (257, 300, 515), (300, 513, 96), (1000, 40, 260), (520, 776, 1544)]
+         (130, 70, 1), (257, 300, 515), (300, 513, 96), (1000, 40, 260), (520, 776, 1544),
+         (1025, 1100, 130), (1111, 1300, 385), (1300, 2050, 1000)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -72,6 +73,36 @@ def test_products(op, M, N, K):
     for dt in (torch.float32, torch.bfloat16):
         gu.announce(f"mx gemm {op} {M}x{N}x{K} {dt}")
         check(fq.fq_mx_gemm(OPS[op], A, B, out_dtype=dt), a, b)
+
+
+# (compute units the planner is told of, M, N, K, the tiles that follow): workgroups that walk over several tiles, edges
+# in both directions, contractions of one block and of odd and even numbers of them, shorter than the ring of stages
+TILED = [(1, 512, 512, 2048, fq.FQ_MX_FORM_256x256), (2, 700, 900, 2100, fq.FQ_MX_FORM_256x256),
+         (1, 500, 1020, 1921, fq.FQ_MX_FORM_256x256), (3, 1000, 530, 1700, fq.FQ_MX_FORM_256x256),
+         (1, 1024, 1024, 100, fq.FQ_MX_FORM_256x256), (1, 1000, 1010, 300, fq.FQ_MX_FORM_256x256),
+         (256, 4090, 4096, 1000, fq.FQ_MX_FORM_256x256),
+         (1, 300, 300, 100, fq.FQ_MX_FORM_128x128), (1, 129, 400, 1, fq.FQ_MX_FORM_128x128),
+         (2, 400, 333, 256, fq.FQ_MX_FORM_128x128), (1, 257, 131, 300, fq.FQ_MX_FORM_128x128),
+         (3, 500, 420, 513, fq.FQ_MX_FORM_128x128), (1, 140, 1000, 700, fq.FQ_MX_FORM_256x256),
+         (1, 70, 1000, 700, fq.FQ_MX_FORM_128x128), (8, 130, 150, 900, fq.FQ_MX_FORM_64x64),
+         (4, 60, 500, 600, fq.FQ_MX_FORM_64x64), (4, 30, 500, 600, fq.FQ_MX_FORM_32x64),
+         (4, 100, 60, 1200, fq.FQ_MX_FORM_32x64)]
+
+
+@pytest.mark.parametrize("cus,M,N,K,tiles", TILED)
+def test_tiles(cus, M, N, K, tiles, monkeypatch):
+    monkeypatch.setenv("FQ_GEMM_CUS", str(cus))
+    assert fq.fq_mx_gemm_form(M, N, K)[0] == tiles
+    op = [fq.FQ_OP_NT, fq.FQ_OP_NN, fq.FQ_OP_TN][(M + N + K) % 3]
+    A, B = pair(op, M, N, K, K)
+    a, b = operands(op, A, B)
+    for dt in (torch.float32, torch.bfloat16):
+        gu.announce(f"mx tiles {tiles} cus {cus} {M}x{N}x{K} {dt}")
+        for ldc in (N, N + 1, N + 8):
+            out = torch.full((M, ldc), 9.0, dtype=dt, device="cuda")
+            fq.fq_mx_gemm(op, A, B, out=out[:, :N])
+            check(out[:, :N], a, b)
+            assert (out[:, N:] == 9.0).all()
 
 
 def test_products_of_small_integers_are_exact():

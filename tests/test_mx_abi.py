@@ -111,6 +111,33 @@ def test_linear_refusals():
     assert f(w, _bind(0, 512), x=None, rows=0, y=None) == fq.FQ_OK
 
 
+def test_form_says_which_tiles_run():
+    form = lambda *a: fq.fq_mx_gemm_form(*a, 256)
+    for M, N, K, want in [(1, 11008, 4096, (fq.FQ_MX_FORM_32x64, True)), (16, 4096, 11008, (fq.FQ_MX_FORM_32x32, False)),
+                          (256, 512, 512, (fq.FQ_MX_FORM_32x32, True)), (256, 1024, 11008, (fq.FQ_MX_FORM_32x32, False)),
+                          (128, 4096, 4096, (fq.FQ_MX_FORM_32x64, False)), (1024, 1024, 4096, (fq.FQ_MX_FORM_64x64, False)),
+                          (64, 11008, 4096, (fq.FQ_MX_FORM_64x64, False)), (1024, 2048, 640, (fq.FQ_MX_FORM_64x64, False)),
+                          (2048, 2048, 2048, (fq.FQ_MX_FORM_128x128, False)), (512, 11008, 128, (fq.FQ_MX_FORM_128x128, False)),
+                          (1500, 11008, 4096, (fq.FQ_MX_FORM_128x128, False)), (4096, 11008, 4096, (fq.FQ_MX_FORM_256x256, False)),
+                          (8192, 8192, 8192, (fq.FQ_MX_FORM_256x256, False)), (3000, 3000, 2048, (fq.FQ_MX_FORM_256x256, False)),
+                          (16, 2 ** 20, 256, (fq.FQ_MX_FORM_32x64, True)), (2 ** 20, 40, 256, (fq.FQ_MX_FORM_64x64, False)),
+                          (0, 5, 5, (0, False)), (4096, 4096, 0, (fq.FQ_MX_FORM_64x64, False))]:
+        assert form(M, N, K) == want, (M, N, K, form(M, N, K))
+    # a linear layer in one launch has the sums of the product of stored codes: 8 parts of the contraction
+    for M in (1, 5, 16, 17, 40, 128, 300):
+        for N in (1, 64, 1000, 4096, 20000, 300000):
+            for K in (32, 512, 4096, 65536, 10 ** 6):
+                tiles, one = form(M, N, K)
+                assert not one or tiles in (fq.FQ_MX_FORM_32x32, fq.FQ_MX_FORM_32x64)
+                assert M > fq.FQ_MX_LINEAR_ROWS or tiles in (fq.FQ_MX_FORM_32x32, fq.FQ_MX_FORM_32x64)
+    assert fq.fq_mx_gemm_form(512, 512, 2048, 1)[0] == fq.FQ_MX_FORM_256x256
+    assert fq.fq_mx_gemm_form(300, 300, 256, 1)[0] == fq.FQ_MX_FORM_128x128
+    p = (C.c_int32 * 2)()
+    for bad in [(-1, 5, 5), (5, -1, 5), (5, 5, -1)]:
+        assert fq.lib().fq_mx_gemm_form(*bad, 4, p) == fq.FQ_ERR_SHAPE
+    assert fq.lib().fq_mx_gemm_form(5, 5, 5, 4, None) == fq.FQ_ERR_NULL
+
+
 class _Recorder:
     def __init__(self):
         self.calls = []
