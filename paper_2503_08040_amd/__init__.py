@@ -241,6 +241,9 @@ def _native_setup():
         _fqnative.setup(*(C.cast(f, C.c_void_p).value for f in (_native_lib.fq_quantize, _native_lib.fq_quantize_sr,
                                                                  _native_lib.fq_gemm)), device, raw)
         _native = _fqnative
+        if hasattr(_fqnative, "setup_mx"):
+            names = ("quantize", "quantize_sr", "dequantize", "gemm", "linear")
+            _fqnative.setup_mx(*(C.cast(getattr(_native_lib, "fq_mx_" + n), C.c_void_p).value for n in names))
 
 
 def _stream_ptr(stream):
@@ -610,6 +613,9 @@ class MxTensor:
         base = (self.storage.data_ptr() + 255) & ~255
         self.c = fq_mx_tensor()
         self._ref = C.byref(self.c)
+        self._addr = C.addressof(self.c)
+        if _native_lib is None:
+            _native_setup()
         _check(lib().fq_mx_bind(C.c_void_p(base), self.rows, self.cols, self.sides, self._ref), "fq_mx_bind")
 
     def view(self, field):
@@ -629,24 +635,44 @@ def fq_mx_bytes(rows, cols, sides=FQ_MX_ROWS) -> int:
     return int(lib().fq_mx_bytes(rows, cols, sides))
 
 
+def _mx_stream(stream, *tensors):
+    """The handle of the stream to launch on (the current one if none is given), on whose device every tensor has to be."""
+    device = _t().cuda.current_device() if stream is None else stream.device_index
+    assert all(t.is_cuda and t.get_device() == device for t in tensors)
+    return _stream_ptr(stream)
+
+
 def fq_mx_quantize(x, out: MxTensor = None, sides=FQ_MX_ROWS, rule=FQ_MX_FLOOR, stream=None) -> MxTensor:
     """x (as for fq_quantize) in microscaled 4 bits, along its rows, its columns or both; into `out` if given, whose
     sides then count."""
+    if _native and stream is None and out is not None and _lib is _native_lib:
+        status = _native.mx_quantize(x, rule, out._addr, out.storage)
+        if status is not None:
+            if status:
+                raise FqError(status, "fq_mx_quantize")
+            return out
     rows, cols, ld = _bf16_matrix(x)
     if out is None:
         out = MxTensor(rows, cols, sides, x.device)
-    _check((_lib or lib()).fq_mx_quantize(x.data_ptr(), rows, cols, ld, int(rule), out._ref, _stream_ptr(stream)),
-           "fq_mx_quantize")
+    st = _mx_stream(stream, x, out.storage)
+    _check((_lib or lib()).fq_mx_quantize(x.data_ptr(), rows, cols, ld, int(rule), out._ref, st), "fq_mx_quantize")
     return out
 
 
 def fq_mx_quantize_sr(x, seed, out: MxTensor = None, sides=FQ_MX_ROWS, stream=None) -> MxTensor:
     """As fq_mx_quantize with stochastic rounding and scales that cover every value."""
+    if _native and stream is None and out is not None and _lib is _native_lib:
+        status = _native.mx_quantize_sr(x, seed, out._addr, out.storage)
+        if status is not None:
+            if status:
+                raise FqError(status, "fq_mx_quantize_sr")
+            return out
     rows, cols, ld = _bf16_matrix(x)
     if out is None:
         out = MxTensor(rows, cols, sides, x.device)
-    _check((_lib or lib()).fq_mx_quantize_sr(x.data_ptr(), rows, cols, ld, C.c_uint64(seed), out._ref,
-                                             _stream_ptr(stream)), "fq_mx_quantize_sr")
+    st = _mx_stream(stream, x, out.storage)
+    _check((_lib or lib()).fq_mx_quantize_sr(x.data_ptr(), rows, cols, ld, C.c_uint64(seed), out._ref, st),
+           "fq_mx_quantize_sr")
     return out
 
 
@@ -655,23 +681,35 @@ def _output(out, shape, out_dtype, device):
     torch = _t()
     if out is None:
         out = torch.empty(shape, dtype=out_dtype, device=device)
-    assert out.is_cuda and out.shape == shape
+    assert out.shape == shape
     return out, {torch.float32: FQ_OUT_F32, torch.bfloat16: FQ_OUT_BF16}[out.dtype], _pitch(out)
 
 
 def fq_mx_dequantize(t: MxTensor, side=FQ_MX_ROWS, out=None, out_dtype=None, stream=None):
     """What the elements of one side stand for: a [rows, cols] bfloat16 (or float32) CUDA tensor."""
+    if _native and stream is None and _lib is _native_lib:
+        r = _native.mx_dequantize(t._addr, t.storage, side, out, out_dtype)
+        if r is not None:
+            if r[0]:
+                raise FqError(r[0], "fq_mx_dequantize")
+            return r[1]
     out, odt, ldo = _output(out, (t.rows, t.cols), out_dtype or _t().bfloat16, t.storage.device)
-    _check((_lib or lib()).fq_mx_dequantize(t._ref, int(side), out.data_ptr(), odt, ldo, _stream_ptr(stream)),
-           "fq_mx_dequantize")
+    st = _mx_stream(stream, t.storage, out)
+    _check((_lib or lib()).fq_mx_dequantize(t._ref, int(side), out.data_ptr(), odt, ldo, st), "fq_mx_dequantize")
     return out
 
 
 def fq_mx_gemm(op, A: MxTensor, B: MxTensor, out=None, out_dtype=None, stream=None):
     """C = A (op) B of microscaled operands; out is a 2-D float32 or bfloat16 CUDA tensor."""
+    if _native and stream is None and _lib is _native_lib:
+        r = _native.mx_gemm(op, A._addr, B._addr, A.storage, B.storage, out, out_dtype)
+        if r is not None:
+            if r[0]:
+                raise FqError(r[0], "fq_mx_gemm")
+            return r[1]
     out, cdt, ldc = _output(out, gemm_out_shape(op, A, B), out_dtype or _t().float32, A.storage.device)
-    _check((_lib or lib()).fq_mx_gemm(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, _stream_ptr(stream)),
-           "fq_mx_gemm")
+    st = _mx_stream(stream, A.storage, B.storage, out)
+    _check((_lib or lib()).fq_mx_gemm(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, st), "fq_mx_gemm")
     return out
 
 
@@ -686,12 +724,19 @@ def fq_mx_gemm_form(rows_out, cols_out, contraction, compute_units=0):
 def fq_mx_linear(x, W: MxTensor, xq: MxTensor = None, rule=FQ_MX_FLOOR, out=None, out_dtype=None, stream=None):
     """Y = Q(x) W^T for a bf16 x and a quantized W; xq is space for Q(x), taken if x has more than FQ_MX_LINEAR_ROWS rows
     and none is given."""
+    if _native and stream is None and _lib is _native_lib:
+        r = _native.mx_linear(x, W._addr, W.storage, xq._addr if xq else 0, xq.storage if xq else None, rule, out, out_dtype)
+        if r is not None:
+            if r[0]:
+                raise FqError(r[0], "fq_mx_linear")
+            return r[1]
     rows, cols, ld = _bf16_matrix(x)
     if cols != W.cols:
         raise FqError(FQ_ERR_SHAPE, "fq_mx_linear")
     if xq is None and rows > FQ_MX_LINEAR_ROWS:
         xq = MxTensor(rows, cols, FQ_MX_ROWS, x.device)
     out, ydt, ldy = _output(out, (rows, W.rows), out_dtype or _t().float32, x.device)
-    _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref if xq else None, out.data_ptr(), ydt,
-                                        ldy, _stream_ptr(stream)), "fq_mx_linear")
+    st = _mx_stream(stream, x, W.storage, out, *([xq.storage] if xq else []))
+    _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref if xq else None, out.data_ptr(),
+                                        ydt, ldy, st), "fq_mx_linear")
     return out

@@ -268,3 +268,47 @@ def test_a_step_replays_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dw, t), want))
+
+
+def test_native_calls_are_the_ctypes_calls(monkeypatch):
+    """Results, errors, the current stream: the same with and without the native module."""
+    pytest.importorskip("paper_2503_08040_amd._fqnative")
+    x, big = matrix(40, 96, 1), matrix(300, 96, 2)
+    W = fq.fq_mx_quantize(matrix(50, 96, 3), sides=fq.FQ_MX_BOTH)
+    assert fq._native is not None
+    side = torch.cuda.Stream()
+
+    def calls():
+        out = []
+        q, s = fq.MxTensor(40, 96, fq.FQ_MX_BOTH), fq.MxTensor(40, 96, fq.FQ_MX_BOTH)
+        with torch.cuda.stream(side):
+            fq.fq_mx_quantize(x, out=q, rule=fq.FQ_MX_COVER)
+            fq.fq_mx_quantize_sr(x, -1, out=s)
+            for t in (q, s):
+                out += [t.view(f).clone() for f in ("codes", "scales", "codes_t", "scales_t")]
+                out += [fq.fq_mx_dequantize(t), fq.fq_mx_dequantize(t, fq.FQ_MX_COLS, out_dtype=torch.float32)]
+            y = torch.zeros((40, 60), device="cuda")
+            out += [fq.fq_mx_gemm(fq.FQ_OP_NT, q, W), fq.fq_mx_gemm(fq.FQ_OP_NT, s, W, out=y[:, 5:55]), y.clone(),
+                    fq.fq_mx_linear(x, W, xq=q, out_dtype=torch.bfloat16), fq.fq_mx_linear(big, W), fq.fq_mx_linear(x[:1], W)]
+        side.synchronize()
+        return out
+
+    def errors():
+        got = []
+        q = fq.MxTensor(40, 96)
+        for call in (lambda: fq.fq_mx_quantize(x, out=q, rule=5), lambda: fq.fq_mx_quantize(big, out=q),
+                     lambda: fq.fq_mx_quantize_sr(big, 1, out=q), lambda: fq.fq_mx_dequantize(q, fq.FQ_MX_COLS),
+                     lambda: fq.fq_mx_gemm(fq.FQ_OP_TN, q, W), lambda: fq.fq_mx_gemm(9, q, W),
+                     lambda: fq.fq_mx_gemm(fq.FQ_OP_NT, q, W, out_dtype=torch.float16),
+                     lambda: fq.fq_mx_linear(x, W, xq=fq.MxTensor(41, 96)), lambda: fq.fq_mx_linear(x[:, :95], W),
+                     lambda: fq.fq_mx_quantize(x.float(), out=q), lambda: fq.fq_mx_quantize(x.cpu(), out=q),
+                     lambda: fq.fq_mx_quantize_sr(x, 1.5, out=q), lambda: fq.fq_mx_gemm(fq.FQ_OP_NT, q, W, out=x)):
+            with pytest.raises(Exception) as e:
+                call()
+            got.append((type(e.value), str(e.value)))
+        return got
+
+    native, native_errors = calls(), errors()
+    monkeypatch.setattr(fq, "_native", None)
+    assert native_errors == errors()
+    assert all(torch.equal(a, b) for a, b in zip(native, calls()))

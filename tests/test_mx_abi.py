@@ -150,37 +150,99 @@ class _Recorder:
         return call
 
 
+def _tensor(rows, cols, sides=3, device=0):
+    """An MxTensor whose storage says that it is on that GPU."""
+    t = fq.MxTensor(rows, cols, sides, device="cpu")
+    t.keep = t.storage
+    t.storage = types.SimpleNamespace(is_cuda=True, get_device=lambda: device, device="cpu")
+    return t
+
+
+def _matrix(rows, cols, pitch, dtype=torch.bfloat16, device=0):
+    return types.SimpleNamespace(dtype=dtype, is_cuda=True, shape=(rows, cols), dim=lambda: 2, device="cpu",
+                                 stride=lambda d=None: (pitch, 1) if d is None else (pitch, 1)[d], data_ptr=lambda: 256,
+                                 get_device=lambda: device)
+
+
 def test_python_layer(monkeypatch):
-    """Shapes, pitches, types and sides as they reach the library; what the Python functions refuse by themselves."""
-    lib = fq.lib()
+    """Shapes, pitches, types, sides and devices as they reach the library; what the Python functions refuse."""
+    q, w, q1, w1 = _tensor(4, 32), _tensor(6, 32), _tensor(4, 32, device=1), _tensor(6, 32, device=1)
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
     rec = _Recorder()
-    stream = types.SimpleNamespace(cuda_stream=5)
-    tensor = lambda rows, cols, sides=3: fq.MxTensor(rows, cols, sides, device="cpu")
-    q, w, g = tensor(4, 32), tensor(6, 32), tensor(4, 6)
-    x = types.SimpleNamespace(dtype=torch.bfloat16, is_cuda=True, shape=(4, 32), dim=lambda: 2, device="cpu",
-                              stride=lambda: (40, 1), data_ptr=lambda: 256)
     monkeypatch.setattr(fq, "_lib", rec)
+    x = _matrix(4, 32, 40)
     fq.fq_mx_quantize(x, out=q, rule=fq.FQ_MX_COVER, stream=stream)
     fq.fq_mx_quantize_sr(x, 2 ** 40 + 1, out=q, stream=stream)
-    name, args = rec.calls[0]
-    assert name == "fq_mx_quantize" and args[:5] == (256, 4, 32, 40, 1) and args[-1] == 5
-    assert rec.calls[1][1][4].value == 2 ** 40 + 1
-    x.dtype = torch.float32
-    with pytest.raises(AssertionError):
-        fq.fq_mx_quantize(x, out=q, stream=stream)
-    x.dtype, x.shape = torch.bfloat16, (4, 33)
-    with pytest.raises(fq.FqError):
-        fq.fq_mx_linear(x, w, stream=stream)
-    for bad in (torch.empty((4, 6)), torch.empty((6, 4))):          # not on the GPU, wrong shape
+    y = _matrix(4, 6, 11, torch.float32)
+    fq.fq_mx_gemm(fq.FQ_OP_NT, q, w, out=y, stream=stream)
+    fq.fq_mx_dequantize(q, fq.FQ_MX_COLS, out=x, stream=stream)
+    fq.fq_mx_linear(x, w, out=_matrix(4, 6, 7), stream=stream)
+    names, args = zip(*rec.calls)
+    assert names == ("fq_mx_quantize", "fq_mx_quantize_sr", "fq_mx_gemm", "fq_mx_dequantize", "fq_mx_linear")
+    assert all(a[-1] == 5 for a in args)
+    assert args[0][:5] == (256, 4, 32, 40, 1) and args[1][:4] == (256, 4, 32, 40) and args[1][4].value == 2 ** 40 + 1
+    assert args[2][0] == fq.FQ_OP_NT and args[2][3:6] == (256, fq.FQ_OUT_F32, 11)
+    assert args[3][1:5] == (fq.FQ_MX_COLS, 256, fq.FQ_OUT_BF16, 40)
+    assert args[4][:4] == (256, 4, 40, fq.FQ_MX_FLOOR) and args[4][5] is None and args[4][7:9] == (fq.FQ_OUT_BF16, 7)
+    refused = [lambda: fq.fq_mx_quantize(_matrix(4, 32, 40, torch.float32), out=q, stream=stream),
+               lambda: fq.fq_mx_gemm(fq.FQ_OP_NT, q, w, out=torch.empty((4, 6)), stream=stream),      # not on the GPU
+               lambda: fq.fq_mx_gemm(fq.FQ_OP_NT, q, w, out=_matrix(6, 4, 4, torch.float32), stream=stream),
+               # tensors on another device than the stream's
+               lambda: fq.fq_mx_quantize(_matrix(4, 32, 40, device=1), out=q, stream=stream),
+               lambda: fq.fq_mx_quantize_sr(x, 1, out=q1, stream=stream),
+               lambda: fq.fq_mx_gemm(fq.FQ_OP_NT, q, w1, out=y, stream=stream),
+               lambda: fq.fq_mx_gemm(fq.FQ_OP_NT, q, w, out=_matrix(4, 6, 6, torch.float32, 1), stream=stream),
+               lambda: fq.fq_mx_dequantize(q1, out=x, stream=stream),
+               lambda: fq.fq_mx_linear(x, w, xq=q1, out=y, stream=stream),
+               lambda: fq.fq_mx_linear(x, w1, out=y, stream=stream)]
+    for call in refused:
         with pytest.raises(AssertionError):
-            fq.fq_mx_gemm(fq.FQ_OP_NT, q, w, out=bad, stream=stream)
-    with pytest.raises(fq.FqError):
-        fq.fq_mx_gemm(7, q, w, stream=stream)
-    assert len(rec.calls) == 2
-    monkeypatch.setattr(fq, "_lib", lib)
+            call()
+    with pytest.raises(KeyError):
+        fq.fq_mx_gemm(fq.FQ_OP_NT, q, w, out=_matrix(4, 6, 6, torch.float16), stream=stream)
+    for call in (lambda: fq.fq_mx_linear(_matrix(4, 33, 33), w, stream=stream), lambda: fq.fq_mx_gemm(7, q, w, stream=stream)):
+        with pytest.raises(fq.FqError):
+            call()
+    assert len(rec.calls) == 5
+
+
+def test_the_current_device_counts_without_a_stream(monkeypatch):
+    q = _tensor(4, 32)
+    rec = _Recorder()
+    for device, taken in ((0, True), (1, False)):
+        cuda = types.SimpleNamespace(current_device=lambda: device, current_stream=lambda: types.SimpleNamespace(cuda_stream=9))
+        monkeypatch.setattr(fq, "_lib", rec)
+        monkeypatch.setattr(fq, "_torch", types.SimpleNamespace(_C=types.SimpleNamespace(), cuda=cuda, bfloat16=torch.bfloat16))
+        monkeypatch.setattr(fq, "_current_stream", None)
+        n = len(rec.calls)
+        if taken:
+            fq.fq_mx_quantize(_matrix(4, 32, 32), out=q)
+            assert len(rec.calls) == n + 1 and rec.calls[-1][1][-1] == 9
+        else:
+            with pytest.raises(AssertionError):
+                fq.fq_mx_quantize(_matrix(4, 32, 32), out=q)
+            assert len(rec.calls) == n
+
+
+def test_views():
+    q = fq.MxTensor(4, 32, 3, device="cpu")
     assert q.view("codes").shape == (1, 1, 1024) and q.view("scales_t").shape == (1, 1, 256)
-    assert q.view("codes_t").shape == (2, 1, 1024) and tensor(4, 4, 1).view("codes_t") is None
-    assert g.view("codes").data_ptr() == g.c.codes
+    assert q.view("codes_t").shape == (2, 1, 1024) and fq.MxTensor(4, 4, 1, device="cpu").view("codes_t") is None
+    assert q.view("codes").data_ptr() == q.c.codes and q.view("scales_t").data_ptr() == q.c.scales_t
     for bad in [(-1, 4, 1), (4, 4, 0), (4, 4, 4)]:
         with pytest.raises(fq.FqError):
-            tensor(*bad)
+            fq.MxTensor(*bad, device="cpu")
+
+
+def test_the_native_module_leaves_anything_unusual_to_the_python_code():
+    native = pytest.importorskip("paper_2503_08040_amd._fqnative")
+    q, w = fq.MxTensor(4, 8, 3, device="cpu"), fq.MxTensor(6, 8, 3, device="cpu")
+    x = torch.zeros((4, 8), dtype=torch.bfloat16)                    # nothing is on the GPU
+    for first in (x, None, 3, x.float(), x[0], torch.nn.Parameter(x)):
+        assert native.mx_quantize(first, 0, q._addr, q.storage) is None
+        assert native.mx_quantize_sr(first, 1, q._addr, q.storage) is None
+        assert native.mx_linear(first, w._addr, w.storage, 0, None, 0, None, None) is None
+    assert native.mx_gemm("0", q._addr, w._addr, q.storage, w.storage, None, None) is None
+    assert native.mx_dequantize(q._addr, None, 1, None, None) is None
+    with pytest.raises(TypeError):
+        native.setup_mx(1, 2)
