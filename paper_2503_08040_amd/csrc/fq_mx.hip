@@ -17,19 +17,27 @@ namespace fq {
 
 namespace {
 
+typedef float v2f __attribute__((ext_vector_type(2)));
+
 constexpr int kThreads = 256;
 constexpr int kTile = 128;        // rows and columns of a workgroup: whole operands along either axis
 constexpr int kWaveRows = 32;     // of a wavefront: one group along the columns
 
-// Stochastic code of a bf16 value (bits) with 16 random bits: t = |x| / 2^s in units of 2^-17, the step above it is
-// 2^16, 2^17 or 2^18 of them; the sum of t and the random part of a step is cut to whole steps.  A finite group has
-// t <= 6; the minimum is for the others, whose code is dropped.
-__device__ __forceinline__ uint32_t code_sr(uint32_t bits, uint32_t u, float inv) {
-  const float x = __uint_as_float((bits & 0x7FFFu) << 16);
-  const uint32_t t = (uint32_t)fminf(x * inv * 0x1p17f, 0x1p20f);      // the conversion cuts
-  const uint32_t sh = (t >= 1u << 18) + (t >= 1u << 19);
-  const uint32_t q = (t + (u << sh)) >> (16 + sh);     // whole steps: codes 0-4 at sh 0, 4 + q - 2 at 1, 6 + q - 2 at 2
-  return (q + 2u * sh) | ((bits >> 12) & 8u);
+// bf16 half k of a dword as binary32, or random bits in the upper half of a word
+__device__ __forceinline__ uint32_t upper(uint32_t w, int k) { return k ? w & 0xFFFF0000u : w << 16; }
+
+// Stochastic codes of two values, in byte 0.  The conversion adds its random word, as a fraction of a step, to the value
+// and cuts; for the second value it takes the word one bit up.  Either value has 16 bits of its own, so both are
+// converted with the word of one, and the nibbles that were made with the right word are put together.
+__device__ __forceinline__ uint32_t cvt_sr(uint32_t x0, uint32_t x1, uint32_t u0, uint32_t u1, float scale) {
+  const v2f v = {__uint_as_float(x0), __uint_as_float(x1)};
+  const uint32_t first = __builtin_amdgcn_cvt_scalef32_sr_pk_fp4_f32(0u, v, u0, scale, 0);
+  const uint32_t second = __builtin_amdgcn_cvt_scalef32_sr_pk_fp4_f32(0u, v, u1 >> 1, scale, 0);
+  return (first & 0x0Fu) | (second & ~0x0Fu);
+}
+// byte 0 of each
+__device__ __forceinline__ uint32_t bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
 
 struct Random8 { uint32_t w[4]; };
@@ -82,15 +90,17 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint32_t byte = scale_byte(k ? m >> 16 : m & 0xFFFFu, p.bias);
+        const float s = scale_value(byte);
         uint32_t c = 0;
         if constexpr (kSr) {
-          const float inv = scale_inverse(byte);
+          uint32_t n[4];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            c |= code_sr((x[i + k][e >> 1] >> (16 * (e & 1))) & 0xFFFFu, (rnd[i + k].w[e >> 1] >> (16 * (e & 1))) & 0xFFFFu,
-                         inv) << (4 * e);
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t v = x[i + k][d], u = rnd[i + k].w[d];
+            n[d] = cvt_sr(upper(v, 0), upper(v, 1), upper(u, 0), upper(u, 1), s);
+          }
+          c = bytes(n[0], n[1], n[2], n[3]);
         } else {
-          const float s = scale_value(byte);
 #pragma unroll
           for (int d = 0; d < 4; ++d) c = cvt_fp4(c, x[i + k][d], s, d);
         }
@@ -113,14 +123,16 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint32_t byte = scale_byte(k ? m >> 16 : m & 0xFFFFu, p.bias);
+        const float s = scale_value(byte);
         uint32_t c = 0;
         if constexpr (kSr) {
-          const float inv = scale_inverse(byte);
+          uint32_t n[4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            c |= code_sr((x[i][d] >> (16 * k)) & 0xFFFFu, (rnd[i].w[d] >> (16 * k)) & 0xFFFFu, inv) << (4 * i);
+          for (int i = 0; i < 4; ++i)
+            n[i] = cvt_sr(upper(x[2 * i][d], k), upper(x[2 * i + 1][d], k), upper(rnd[2 * i].w[d], k),
+                          upper(rnd[2 * i + 1].w[d], k), s);
+          c = bytes(n[0], n[1], n[2], n[3]);
         } else {
-          const float s = scale_value(byte);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             c = cvt_fp4(c, __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], k ? 0x07060302u : 0x05040100u), s, i);

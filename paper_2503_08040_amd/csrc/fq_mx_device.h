@@ -45,11 +45,6 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t m, int bias) {
 // 2^(byte - 127) as the conversions take it; 2^-127 is a subnormal number.
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
 
-// 2^(127 - byte): multiplication by it divides by the scale.
-__device__ __forceinline__ float scale_inverse(uint32_t byte) {
-  return __uint_as_float(byte < 254u ? (254u - byte) << 23 : 0x00400000u);
-}
-
 __device__ __forceinline__ uint32_t cvt_fp4(uint32_t old, uint32_t pair, float scale, int sel) {
   const v2bf v = __builtin_bit_cast(v2bf, pair);
   switch (sel) {
