@@ -42,6 +42,34 @@ __device__ __forceinline__ uint32_t bytes(uint32_t a, uint32_t b, uint32_t c, ui
 
 struct Random8 { uint32_t w[4]; };
 
+// The 8 x 8 values at (row0, col0), packed pairs; what is not there reads as 0.  All loads are requested before one of
+// them is used: behind the edges a lane reads the last row, and the last 8 columns, which it shifts.
+__device__ __forceinline__ void load_rows(const MxQuantParams& p, int row0, int col0, v4u (&x)[8]) {
+  if (p.cols < 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = v4u{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (row0 + i < p.rows && col0 + e < p.cols) x[i][e >> 1] |= (uint32_t)p.x[(row0 + i) * p.ld + col0 + e] << (16 * (e & 1));
+    }
+    return;
+  }
+  const int col = min(col0, p.cols - 8), missing = col0 - col;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const v4u_at2*>(p.x + min(row0 + i, p.rows - 1) * p.ld + col);
+  if (missing | (row0 + 8 > p.rows)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (missing & 4) x[i] = v4u{x[i][2], x[i][3], 0u, 0u};
+      if (missing & 2) x[i] = v4u{x[i][1], x[i][2], x[i][3], 0u};
+      if (missing & 1)
+        x[i] = v4u{x[i][0] >> 16 | x[i][1] << 16, x[i][1] >> 16 | x[i][2] << 16, x[i][2] >> 16 | x[i][3] << 16, x[i][3] >> 16};
+      if (missing >= 8 || row0 + i >= p.rows) x[i] = v4u{0u, 0u, 0u, 0u};
+    }
+  }
+}
+
 template <bool kRows, bool kCols, bool kSr>
 __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t codes_lds[4][2][2 * kOperand];   // wavefront, side
@@ -53,21 +81,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
   const int row0 = bi * kTile + w * kWaveRows + 8 * h, col0 = bk * kTile + 8 * q;
 
   v4u x[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = row0 + i;
-    x[i] = v4u{0u, 0u, 0u, 0u};
-    if (row < p.rows && col0 < p.cols) {
-      const uint16_t* src = p.x + row * p.ld + col0;
-      if (col0 + 8 <= p.cols) {
-        x[i] = *reinterpret_cast<const v4u_at2*>(src);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (col0 + e < p.cols) x[i][e >> 1] |= (uint32_t)src[e] << (16 * (e & 1));
-      }
-    }
-  }
+  load_rows(p, row0, col0, x);
   Random8 rnd[kSr ? 8 : 1];
   if constexpr (kSr) {
 #pragma unroll
@@ -181,6 +195,29 @@ __device__ __forceinline__ uint32_t cvt_bf16(uint32_t codes, float scale, int se
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// Byte k of 8 dwords, 16-byte aligned.
+__device__ __forceinline__ void load_bytes(const uint8_t* src, int k, uint32_t (&byte)[8]) {
+  const v4u lo = reinterpret_cast<const v4u*>(src)[0], hi = reinterpret_cast<const v4u*>(src)[1];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) byte[i] = (i < 4 ? lo[i & 3] : hi[i & 3]) >> (8 * k) & 255u;
+}
+
+// Dword k of lane row h (16 lanes each) becomes dword h of lane row k.
+__device__ __forceinline__ void transpose_rows(v4u& v) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const v2u s = __builtin_amdgcn_permlane32_swap(v[k], v[k + 2], false, false);
+    v[k] = s[0];
+    v[k + 2] = s[1];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; k += 2) {
+    const v2u s = __builtin_amdgcn_permlane16_swap(v[k], v[k + 1], false, false);
+    v[k] = s[0];
+    v[k + 1] = s[1];
+  }
+}
+
 // The same split of a tile the other way: a lane takes 8 dwords of codes (8 values each) and has 8 x 8 values.
 template <bool kCols, bool kBf16>
 __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxDequantParams p) {
@@ -189,7 +226,8 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxDequantParams
   const int nbc = (p.cols + kTile - 1) / kTile;
   const int bi = blockIdx.x / nbc, bk = blockIdx.x % nbc;
   const int row0 = bi * kTile + w * kWaveRows + 8 * h, col0 = bk * kTile + 8 * q;
-  if (row0 >= p.rows || col0 >= p.cols) return;
+  // the columns' side exchanges dwords between the rows of a wavefront: those lanes stay together
+  if (col0 >= p.cols || (kCols ? bi * kTile + w * kWaveRows : row0) >= p.rows) return;
   constexpr uint32_t kNan = 0x7FC07FC0u;
   uint32_t y[8][4];          // bf16 pairs
   if constexpr (!kCols) {
@@ -197,11 +235,10 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxDequantParams
     const int64_t at = (int64_t)strip * p.s.nkb + bk;
     const int64_t sat = (int64_t)(strip >> 2) * p.s.nkb + bk;
     uint32_t c[8], byte[8];
+    const uint8_t* const src = p.s.codes + at * kOperand + (r + 16 * (q >> 2)) * 16 + 4 * (q & 3);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      c[i] = *reinterpret_cast<const uint32_t*>(p.s.codes + at * kOperand + (r + i + 16 * (q >> 2)) * 16 + 4 * (q & 3));
-      byte[i] = p.s.scales[sat * kScaleBlock + (r + i + 16 * (q >> 2)) * 4 + (strip & 3)];
-    }
+    for (int i = 0; i < 8; ++i) c[i] = *reinterpret_cast<const uint32_t*>(src + i * 16);
+    load_bytes(p.s.scales + sat * kScaleBlock + (r + 16 * (q >> 2)) * 4, strip & 3, byte);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -210,11 +247,17 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxDequantParams
     const int strip = col0 >> 4, r = col0 & 15;
     const int64_t at = (int64_t)strip * p.s.nkb + bi;
     const int64_t sat = (int64_t)(strip >> 2) * p.s.nkb + bi;
+    // the four lanes 16 apart need 8 columns' 16 bytes: each loads two of them, then dword h of all goes to lane h
     uint32_t c[8], byte[8];
+    const v4u* const src = reinterpret_cast<const v4u*>(p.s.codes + at * kOperand + (r + 16 * w) * 16) + 2 * h;
+    v4u a = src[0], b = src[1];
+    load_bytes(p.s.scales + sat * kScaleBlock + (r + 16 * w) * 4, strip & 3, byte);
+    transpose_rows(a);
+    transpose_rows(b);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      c[j] = *reinterpret_cast<const uint32_t*>(p.s.codes + at * kOperand + (r + j + 16 * w) * 16 + 4 * h);
-      byte[j] = p.s.scales[sat * kScaleBlock + (r + j + 16 * w) * 4 + (strip & 3)];
+    for (int j = 0; j < 4; ++j) {
+      c[2 * j] = a[j];
+      c[2 * j + 1] = b[j];
     }
 #pragma unroll
     for (int d = 0; d < 4; ++d)
