@@ -146,6 +146,7 @@ struct MxQuantParams {
   int stochastic;
   uint64_t seed;
   MxSide r, t;         // along the rows, along the columns
+  int apart;           // filled in by launch_mx_quantize: two workgroups a tile, one for each of the sides
 };
 
 struct MxDequantParams {

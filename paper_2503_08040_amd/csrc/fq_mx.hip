@@ -58,15 +58,20 @@ __device__ __forceinline__ void load_rows(const MxQuantParams& p, int row0, int 
   const int col = min(col0, p.cols - 8), missing = col0 - col;
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const v4u_at2*>(p.x + min(row0 + i, p.rows - 1) * p.ld + col);
-  if (missing | (row0 + 8 > p.rows)) {
+  if (missing) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (missing & 4) x[i] = v4u{x[i][2], x[i][3], 0u, 0u};
       if (missing & 2) x[i] = v4u{x[i][1], x[i][2], x[i][3], 0u};
       if (missing & 1)
         x[i] = v4u{x[i][0] >> 16 | x[i][1] << 16, x[i][1] >> 16 | x[i][2] << 16, x[i][2] >> 16 | x[i][3] << 16, x[i][3] >> 16};
-      if (missing >= 8 || row0 + i >= p.rows) x[i] = v4u{0u, 0u, 0u, 0u};
+      if (missing >= 8) x[i] = v4u{0u, 0u, 0u, 0u};
     }
+  }
+  if (row0 + 8 > p.rows) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (row0 + i >= p.rows) x[i] = v4u{0u, 0u, 0u, 0u};
   }
 }
 
@@ -77,7 +82,9 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int h = lane >> 4, q = lane & 15;
   const int nbc = p.r.nkb;                               // tiles across
-  const int bi = blockIdx.x / nbc, bk = blockIdx.x % nbc;
+  const int tile = kRows && kCols ? blockIdx.x >> p.apart : blockIdx.x;
+  const int bi = tile / nbc, bk = tile % nbc;
+  const bool rows = kRows && !(kCols && p.apart && (blockIdx.x & 1)), cols = kCols && !(kRows && p.apart && !(blockIdx.x & 1));
   const int row0 = bi * kTile + w * kWaveRows + 8 * h, col0 = bk * kTile + 8 * q;
 
   v4u x[8];
@@ -90,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
   }
   constexpr uint32_t kMag = 0x7FFF7FFFu;
 
-  if constexpr (kRows) {
+  if (rows) {
     uint8_t* const lds = codes_lds[w][0];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
@@ -126,7 +133,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
       }
     }
   }
-  if constexpr (kCols) {
+  if (cols) {
     uint8_t* const lds = codes_lds[w][1];
 #pragma unroll
     for (int d = 0; d < 4; ++d) {                        // columns 2 d and 2 d + 1 of the lane's 8
@@ -162,13 +169,13 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
 
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    if constexpr (kRows) {
+    if (rows) {
       const int strip = bi * 8 + w * 2 + u;
       if (strip < p.r.strips)
         *reinterpret_cast<v4u*>(p.r.codes + ((int64_t)strip * p.r.nkb + bk) * kOperand + lane * 16) =
             *reinterpret_cast<const v4u*>(codes_lds[w][0] + u * kOperand + lane * 16);
     }
-    if constexpr (kCols) {
+    if (cols) {
       const int c = lane + 64 * u, strip = bk * 8 + (c >> 4);
       if (strip < p.t.strips)
         *reinterpret_cast<v4u*>(p.t.codes + ((int64_t)strip * p.t.nkb + bi) * kOperand + w * 256 + (c & 15) * 16) =
@@ -176,10 +183,10 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxQuantParams p) 
     }
   }
   const int half = w & 1;
-  if (kRows && w < 2 && 2 * bi + half < p.r.quads)
+  if (rows && w < 2 && 2 * bi + half < p.r.quads)
     *reinterpret_cast<uint32_t*>(p.r.scales + ((int64_t)(2 * bi + half) * p.r.nkb + bk) * kScaleBlock + lane * 4) =
         *reinterpret_cast<const uint32_t*>(&scales_lds[0][half][lane * 4]);
-  if (kCols && w >= 2 && 2 * bk + half < p.t.quads)
+  if (cols && w >= 2 && 2 * bk + half < p.t.quads)
     *reinterpret_cast<uint32_t*>(p.t.scales + ((int64_t)(2 * bk + half) * p.t.nkb + bi) * kScaleBlock + lane * 4) =
         *reinterpret_cast<const uint32_t*>(&scales_lds[1][half][lane * 4]);
 }
@@ -313,8 +320,14 @@ void quantize_sides(const MxQuantParams& p, dim3 grid, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_mx_quantize(const MxQuantParams& p, hipStream_t st) {
-  const dim3 grid(tiles(p.rows, p.cols));
+// Few tiles are quantized along either axis by a workgroup each: what counts then is how long one takes (131 x 2200
+// stochastic 6.0 -> 5.0 us).  From more than 128 tiles on they would not all run at once and read x twice (1536 x 2048
+// 5.5 us instead of 4.9).
+hipError_t launch_mx_quantize(const MxQuantParams& given, hipStream_t st) {
+  MxQuantParams p = given;
+  const int n = tiles(p.rows, p.cols);
+  p.apart = p.r.codes && p.t.codes && n <= 128 ? 1 : 0;
+  const dim3 grid(n << p.apart);
   if (p.stochastic) quantize_sides<true>(p, grid, st);
   else quantize_sides<false>(p, grid, st);
   return hipGetLastError();

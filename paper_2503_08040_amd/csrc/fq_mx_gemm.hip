@@ -223,11 +223,11 @@ __device__ __forceinline__ void mfma_in_place_select(v4f& acc, const v4i& a, con
 // global -> LDS loads.  There are kStages of them: while a block is multiplied out of registers, the next one's operands
 // are fetched from LDS and up to three more blocks are under way.  A workgroup walks over several tiles and the ring of
 // stages runs on from one to the next, so that only the first tile waits for its operands.
-template <int kR_, int kC_, int kWC_, int kOcc_>
+template <int kR_, int kC_, int kWC_, int kOcc_, int kStages_>
 struct LdsGeo {
   static constexpr int kR = kR_, kC = kC_, kWC = kWC_, kOcc = kOcc_;        // strips of a wavefront; workgroups of a CU
   static constexpr int kWaves = 2 * kWC, kThreads = 64 * kWaves;
-  static constexpr int kStages = 4;
+  static constexpr int kStages = kStages_;
   static constexpr int kStrips = 2 * kR;                                    // of the tile along either axis
   static constexpr int kLoads = kStrips * 2 / kWaves;                       // strips that a wavefront loads
   static constexpr int kQuads = kStrips / 4, kScaleLoads = kQuads * 2 / kWaves;   // 64 rows' scales along an axis; loads of them
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
   // a block out of `o`, the next one into `other`
   auto block = [&](const Operands& o, Operands& other) {
     // the next block is there, and everybody has this one's operands in registers, so its stage is free
-    wait_stages(std::integral_constant<int, 2>{});
+    wait_stages(std::integral_constant<int, G::kStages - 2>{});
     asm volatile("s_barrier" ::: "memory");
 #pragma unroll
     for (int i = 0; i < kR; ++i)
@@ -518,8 +518,8 @@ hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st) {
     case MxForm::k32x32: return split<2, 2, 8, 2, false>(p, st);
     case MxForm::k32x64: return split<2, 4, 8, 2, false>(p, st);
     case MxForm::k64x64: return split<4, 4, 4, 2, false>(p, st);
-    case MxForm::k128x128: return through_lds<LdsGeo<4, 4, 2, 2>>(p, cus, st);
-    case MxForm::k256x256: return through_lds<LdsGeo<8, 4, 4, 1>>(p, cus, st);
+    case MxForm::k128x128: return through_lds<LdsGeo<4, 4, 2, 2, 4>>(p, cus, st);
+    case MxForm::k256x256: return through_lds<LdsGeo<8, 4, 4, 1, 4>>(p, cus, st);
   }
   return hipErrorInvalidValue;
 }
