@@ -64,9 +64,9 @@ __device__ inline void philox4x32_10(uint32_t c0, uint32_t c1, uint32_t k0, uint
     const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
     const uint32_t h0 = (uint32_t)(p0 >> 32), l0 = (uint32_t)p0;
     const uint32_t h1 = (uint32_t)(p1 >> 32), l1 = (uint32_t)p1;
-    c0 = h1 ^ c1 ^ k0;
+    c0 = __builtin_amdgcn_bitop3_b32(h1, c1, k0, 0x96);      // a ^ b ^ c
     c1 = l1;
-    c2 = h0 ^ c3 ^ k1;
+    c2 = __builtin_amdgcn_bitop3_b32(h0, c3, k1, 0x96);
     c3 = l0;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
