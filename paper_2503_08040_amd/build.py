@@ -3,6 +3,7 @@ import hashlib
 import importlib.util
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -74,8 +75,9 @@ def build_tools() -> list:
 
 
 # Ablation builds of the GEMM kernel (measurement support, see the switches at the top of
-# csrc/fq_gemm.hip): whole libraries, libfq_ablate_<name>.so, loaded instead of libfq.so when the
+# csrc/fq_gemm.hip, the one source that has any): whole libraries, libfq_ablate_<name>.so, loaded instead of libfq.so when the
 # environment variable FQ_LIBRARY names one.  They compute wrong products on purpose.
+ABLATED = "fq_gemm.hip"
 ABLATIONS = {
     "no_dma": ["-DFQ_ABLATE_NO_DMA"],
     "no_multiply": ["-DFQ_ABLATE_NO_MULTIPLY"],
@@ -99,16 +101,24 @@ def build_ablations(names=None, jobs: int = 6) -> list:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     names = list(ABLATIONS) if names is None else list(names)
 
-    def one(name):
-        cmd = [hipcc] + HIPCC_FLAGS + [header_flag(), "-Wno-unused-but-set-variable", "-Wno-unused-variable"] + \
-              ABLATIONS[name] + ["-o", ablation_lib(name)] + [os.path.join(CSRC, f) for f in SOURCES]
+    flags = [hipcc] + HIPCC_FLAGS + [header_flag(), "-Wno-unused-but-set-variable", "-Wno-unused-variable"]
+
+    def run(cmd, name):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"hipcc failed ({name}):\n{r.stderr}")
+
+    def one(name, objects):
+        run(flags + ABLATIONS[name] + ["-o", ablation_lib(name), os.path.join(CSRC, ABLATED)] + objects, name)
         return ablation_lib(name)
 
-    with ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
-        return list(ex.map(one, names))
+    # the sources without switches are the same in all of them
+    with ThreadPoolExecutor(max_workers=max(1, jobs)) as ex, tempfile.TemporaryDirectory() as tmp:
+        common = [f for f in SOURCES if f != ABLATED]
+        objects = [os.path.join(tmp, f + ".o") for f in common]
+        compile_only = [f for f in flags if f != "-shared"]
+        list(ex.map(lambda f, o: run(compile_only + ["-c", "-o", o, os.path.join(CSRC, f)], f), common, objects))
+        return list(ex.map(lambda name: one(name, objects), names))
 
 
 def _older(target, deps) -> bool:
