@@ -517,7 +517,8 @@ fq_status fq_mx_dequantize(const fq_mx_tensor *t, int32_t side, void *out, fq_ou
  * scales are exact and are added in binary32, in an order that depends on the shapes only; stored
  * as binary32 or rounded once to bf16.  A group of scale byte 255 makes every output it enters NaN.
  * C, ldc and errors as fq_gemm (FQ_ERR_NULL: also a side that the product needs and the tensor does
- * not keep); FQ_ERR_SHAPE also for an output of more than 2^23 tiles of 64 x 64.
+ * not keep); FQ_ERR_SHAPE also for an output of more than 2^23 tiles of 64 x 64, or,
+ * where it has 64 rows or columns at most, of 2^21.
  */
 fq_status fq_mx_gemm(fq_op op, const fq_mx_tensor *A, const fq_mx_tensor *B, void *C, fq_out_dtype cdt,
                      int64_t ldc, void *hip_stream);
@@ -542,8 +543,9 @@ fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contractio
  * `rule`, and W quantized before (rows' side, [N, K], K = X's columns).  The same values, bit for
  * bit, as fq_mx_quantize into `xq` and fq_mx_gemm; for few rows in one launch that quantizes X on
  * its way into the product.  xq: a tensor of X's shape that keeps its rows' side, whose contents
- * are unspecified afterwards; up to FQ_MX_LINEAR_ROWS rows it may be NULL.
- * Errors as those two calls.
+ * are unspecified afterwards (calls and captured graphs that share it must be ordered); up to
+ * FQ_MX_LINEAR_ROWS rows it may be NULL.
+ * Errors as those two calls; FQ_ERR_SHAPE also for W's own codes or scales as xq's.
  */
 #define FQ_MX_LINEAR_ROWS 16
 fq_status fq_mx_linear(const void *x_bf16, int32_t rows, int64_t ld, fq_mx_rule rule, const fq_mx_tensor *W,

@@ -735,6 +735,8 @@ def fq_mx_linear(x, W: MxTensor, xq: MxTensor = None, rule=FQ_MX_FLOOR, out=None
         raise FqError(FQ_ERR_SHAPE, "fq_mx_linear")
     if xq is None and rows > FQ_MX_LINEAR_ROWS:
         xq = MxTensor(rows, cols, FQ_MX_ROWS, x.device)
+        if stream is not None:
+            xq.storage.record_stream(stream)        # its memory is given back when this returns
     out, ydt, ldy = _output(out, (rows, W.rows), out_dtype or _t().float32, x.device)
     st = _mx_stream(stream, x, W.storage, out, *([xq.storage] if xq else []))
     _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref if xq else None, out.data_ptr(),

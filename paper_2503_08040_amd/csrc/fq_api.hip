@@ -477,6 +477,7 @@ fq_status fq_gemm_plain(fq_op op, const fq_qtensor* A, const fq_qtensor* B, void
 
 namespace {
 constexpr int64_t kMxMaxBlocks = (int64_t)1 << 23;   // of 128 x 128: the launches count them, 256 threads each, in 32 bits
+constexpr int64_t kMxMaxNarrow = (int64_t)1 << 21;   // tiles of 64 x 64 that may be cut into 32 x 32 of 512 threads
 constexpr int kMxOperandBytes = 1024, kMxScaleBytes = 256;
 
 bool mx_shape_ok(int32_t rows, int32_t cols) {
@@ -535,7 +536,8 @@ fq_status prepare_mx_gemm(fq_op op, const fq_mx_tensor* A, const fq_mx_tensor* B
   if (!g->a.codes || !g->b.codes) return FQ_ERR_NULL;
   g->M = a_t ? A->cols : A->rows;
   g->N = b_t ? B->cols : B->rows;
-  if (ldc < g->N || (int64_t)g->a.quads * g->b.quads > kMxMaxBlocks) return FQ_ERR_SHAPE;
+  const bool narrow = g->a.quads <= 1 || g->b.quads <= 1;
+  if (ldc < g->N || (int64_t)g->a.quads * g->b.quads > (narrow ? kMxMaxNarrow : kMxMaxBlocks)) return FQ_ERR_SHAPE;
   if (g->M == 0 || g->N == 0) return FQ_OK;
   if (!C) return FQ_ERR_NULL;
   g->c = C; g->ldc = ldc; g->out_bf16 = cdt == FQ_OUT_BF16;
@@ -633,6 +635,7 @@ fq_status fq_mx_linear(const void* x_bf16, int32_t rows, int64_t ld, fq_mx_rule 
     const fq_status s = check_mx(xq);
     if (s != FQ_OK) return s;
     if (xq->rows != rows || xq->cols != W->cols) return FQ_ERR_SHAPE;
+    if (xq->codes && (xq->codes == W->codes || xq->scales == W->scales)) return FQ_ERR_SHAPE;
     side.codes = xq->codes;
     side.scales = xq->scales;
   } else if (rows > FQ_MX_LINEAR_ROWS) {

@@ -427,7 +427,10 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
           if constexpr (sizeof(T) == 2) *reinterpret_cast<v2u*>(dst) = pack_bf16(acc[i][jj + j]);
           else *reinterpret_cast<v4f*>(dst) = acc[i][jj + j];
         }
+        // lanes read what others of the wavefront wrote: LDS serves a wavefront in order, the compiler is told to
+        asm volatile("" ::: "memory");
         store_patch<kChunks, T>(p, patch, (i0 + wr * kR + i) * 16, (j0 + wc * kC + jj) * 16, lane);
+        asm volatile("" ::: "memory");
       }
   }
   wait_stages(std::integral_constant<int, 0>{});      // nothing may be under way into LDS when the workgroup ends
@@ -462,10 +465,6 @@ hipError_t split(const MxGemmParams& p, hipStream_t st) {
   hipLaunchKernelGGL((mx_gemm_split_kernel<kM, kN, kW, kU, kFused>), dim3(ti * tj), dim3(64 * kW), 0, st, p, tj);
   return hipGetLastError();
 }
-
-}  // namespace
-
-namespace {
 
 int64_t tiles_of(int M, int N, int rows, int cols) {
   return (int64_t)((M + rows - 1) / rows) * ((N + cols - 1) / cols);

@@ -105,6 +105,15 @@ def test_tiles(cus, M, N, K, tiles, monkeypatch):
             assert (out[:, N:] == 9.0).all()
 
 
+@pytest.mark.parametrize("n,k", [(40, 300), (400, 400), (700, 700)])
+def test_a_matrix_with_itself(n, k):
+    """One tensor as both operands, either side."""
+    q = fq.fq_mx_quantize(matrix(n, k, 4), sides=fq.FQ_MX_BOTH)
+    for op in OPS if n == k else ("NT", "TN"):
+        gu.announce(f"mx product of a {n} x {k} matrix with itself, op {op}")
+        check(fq.fq_mx_gemm(OPS[op], q, q), *operands(OPS[op], q, q))
+
+
 def test_products_of_small_integers_are_exact():
     """Whole numbers up to 6 at scale 1 and sums below 2^24: nothing may round."""
     g = torch.Generator(device="cuda")
@@ -312,3 +321,27 @@ def test_native_calls_are_the_ctypes_calls(monkeypatch):
     monkeypatch.setattr(fq, "_native", None)
     assert native_errors == errors()
     assert all(torch.equal(a, b) for a, b in zip(native, calls()))
+
+
+def test_far_offsets():
+    """More than 2^31 elements: the last block row of the quantizer, of what is read back and of a product against the
+    same calls on that block row alone, bit for bit."""
+    rows, cols, first = 70000, 40960, 546 * 128
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    for r in range(0, rows, 7000):
+        x[r:r + 7000] = matrix(min(7000, rows - r), cols, r)
+    gu.announce("mx quantize of more than 2^31 elements")
+    q, part = fq.fq_mx_quantize(x, sides=fq.FQ_MX_BOTH), fq.fq_mx_quantize(x[first:], sides=fq.FQ_MX_BOTH)
+    assert torch.equal(q.view("codes")[first // 16:], part.view("codes"))
+    assert torch.equal(q.view("scales")[first // 64:], part.view("scales"))
+    assert torch.equal(q.view("codes_t")[:, first // 128:], part.view("codes_t"))
+    assert torch.equal(q.view("scales_t")[:, first // 128:], part.view("scales_t"))
+    for side in (fq.FQ_MX_ROWS, fq.FQ_MX_COLS):
+        assert torch.equal(fq.fq_mx_dequantize(q, side)[first:], fq.fq_mx_dequantize(part, side))
+    del q, part
+    A, tail, B = (fq.fq_mx_quantize(t) for t in (x[:, :100], x[first:, :100], x[:cols, 100:200]))
+    gu.announce("mx product of more than 2^31 elements")
+    y = fq.fq_mx_gemm(fq.FQ_OP_NT, A, B, out_dtype=torch.bfloat16)
+    # one block of 128: a single matrix instruction per output, whatever the tiles
+    assert torch.equal(y[first:], fq.fq_mx_gemm(fq.FQ_OP_NT, tail, B, out_dtype=torch.bfloat16))
+    assert torch.equal(y[:50], fq.fq_mx_gemm(fq.FQ_OP_NT, fq.fq_mx_quantize(x[:50, :100]), B, out_dtype=torch.bfloat16))

@@ -95,6 +95,8 @@ def test_gemm_refusals():
         assert g(op, _bind(*shape[0], sa), _bind(*shape[1], sb)) == fq.FQ_ERR_NULL, (op, sa, sb)
     wide = _bind(2 ** 18, 1, rows), _bind(2 ** 18 + 64, 1, rows)       # 2^12 and 2^12 + 1 tiles of 64
     assert g(0, *wide, ldc=2 ** 19) == fq.FQ_ERR_SHAPE
+    long, short = _bind(2 ** 27 + 1, 1, rows), _bind(1, 1, rows)       # 2^21 + 1 tiles of 64, cut into smaller ones
+    assert g(0, long, short, ldc=1) == g(0, short, long, ldc=2 ** 28) == fq.FQ_ERR_SHAPE
     assert g(0, _bind(0, 512), b, None) == g(0, a, _bind(0, 512), None, ldc=0) == fq.FQ_OK
 
 
@@ -103,11 +105,12 @@ def test_linear_refusals():
     ref = lambda t: C.byref(t) if t is not None else None
     f = lambda w, q, x=X, rows=40, ld=512, rule=0, y=X, ydt=0, ldy=384: \
         L.fq_mx_linear(x, rows, ld, rule, ref(w), ref(q), y, ydt, ldy, None)
-    w, q = _bind(384, 512), _bind(40, 512)
+    w, q = _bind(384, 512), _bind(40, 512, base=0x900000)
     assert f(None, q) == f(w, None) == f(w, q, x=None) == f(w, q, y=None) == fq.FQ_ERR_NULL
     assert f(w, q, rule=2) == f(w, q, ydt=2) == fq.FQ_ERR_ENUM
-    assert f(w, q, rows=41) == f(w, q, rows=-1) == f(w, q, ld=511) == f(w, q, ldy=383) == f(w, _bind(40, 513)) == fq.FQ_ERR_SHAPE
-    assert f(_bind(384, 512, fq.FQ_MX_COLS), q) == f(w, _bind(40, 512, fq.FQ_MX_COLS)) == fq.FQ_ERR_NULL
+    assert f(w, q, rows=41) == f(w, q, rows=-1) == f(w, q, ld=511) == f(w, q, ldy=383) == f(w, _bind(40, 513, base=0x900000)) == fq.FQ_ERR_SHAPE
+    assert f(q, q) == fq.FQ_ERR_SHAPE                # the space for Q(X) is W itself
+    assert f(_bind(384, 512, fq.FQ_MX_COLS), q) == f(w, _bind(40, 512, fq.FQ_MX_COLS, 0x900000)) == fq.FQ_ERR_NULL
     assert f(w, _bind(0, 512), x=None, rows=0, y=None) == fq.FQ_OK
 
 
@@ -204,6 +207,21 @@ def test_python_layer(monkeypatch):
         with pytest.raises(fq.FqError):
             call()
     assert len(rec.calls) == 5
+
+
+def test_space_taken_for_a_call_is_kept_for_its_stream(monkeypatch):
+    """The space for Q(x) that fq_mx_linear takes by itself is freed when it returns, while the given stream uses it."""
+    w = _tensor(6, 32)
+    kept = []
+    make = lambda rows, cols, sides, device: types.SimpleNamespace(
+        _ref=None, storage=types.SimpleNamespace(is_cuda=True, get_device=lambda: 0, record_stream=kept.append))
+    monkeypatch.setattr(fq, "_lib", _Recorder())
+    monkeypatch.setattr(fq, "MxTensor", make)
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
+    fq.fq_mx_linear(_matrix(40, 32, 32), w, out=_matrix(40, 6, 6), stream=stream)
+    assert kept == [stream]
+    fq.fq_mx_linear(_matrix(16, 32, 32), w, out=_matrix(16, 6, 6), stream=stream)
+    assert kept == [stream]
 
 
 def test_the_current_device_counts_without_a_stream(monkeypatch):

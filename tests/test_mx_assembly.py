@@ -1,0 +1,95 @@
+"""What the compiler made of csrc/fq_mx_gemm.hip and csrc/fq_mx.hip (gfx950 assembly of this repository's own sources):
+nothing spills, the hand-written loads and matrix instructions keep their wait states, the accumulators stay where they
+are in the loop."""
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2503_08040_amd import build
+
+HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+
+
+@pytest.fixture(scope="module")
+def assembly(tmp_path_factory):
+    if not (os.path.exists(HIPCC) or shutil.which(HIPCC)):
+        pytest.skip("hipcc is not installed")
+    text = {}
+    for name in ("fq_mx", "fq_mx_gemm"):
+        out = tmp_path_factory.mktemp("asm") / f"{name}.s"
+        flags = [f for f in build.HIPCC_FLAGS if f != "-shared"]
+        r = subprocess.run([HIPCC, *flags, "--offload-device-only", "-S", "-o", str(out),
+                            os.path.join(build.CSRC, f"{name}.hip")], capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stderr
+        text[name] = out.read_text()
+    return text
+
+
+def kernels(text):
+    """name -> its instructions, in order."""
+    out = {}
+    for name, body in re.findall(r"^(_Z\S+):\s*;.*?\n(.*?)^\s*s_endpgm", text, flags=re.M | re.S):
+        lines = (ln.split(";")[0].strip() for ln in body.splitlines())
+        out[name] = [ln for ln in lines if ln and not ln.startswith(".") and not ln.endswith(":")]
+    return out
+
+
+def test_registers(assembly):
+    seen = 0
+    for text in assembly.values():
+        for name, size, vgprs, spills in re.findall(
+                r"\.name:\s+(\S+)\n\s+\.private_segment_fixed_size: (\d+)\n(?:.*\n)*?\s+\.vgpr_count:\s+(\d+)\n"
+                r"\s+\.vgpr_spill_count: (\d+)", text):
+            assert (size, spills) == ("0", "0"), name
+            if "mx_gemm_lds" in name:
+                assert int(vgprs) <= 256, name          # two wavefronts on a SIMD
+                seen += 1
+    assert seen == 4
+
+
+def test_direct_loads_keep_their_wait_states(assembly):
+    n = 0
+    for name, code in kernels(assembly["fq_mx_gemm"]).items():
+        for i, s in enumerate(code):
+            if s.startswith("global_load_lds"):
+                # m0, then the base moved by the scalar unit (which is also the wait state behind m0)
+                assert re.fullmatch(r"s_mov_b32 m0, s\d+", code[i - 2]), code[i - 2:i + 1]
+                base = re.fullmatch(r"s_mov_b64 (s\[\d+:\d+\]), \1", code[i - 1])
+                assert base and s.endswith(base.group(1)), code[i - 2:i + 1]
+                n += 1
+    assert n > 40
+
+
+def test_accumulators(assembly):
+    """In place, in order, and not touched between the products; not read before 32 wait states after the last."""
+    checked = 0
+    for name, code in kernels(assembly["fq_mx_gemm"]).items():
+        if "mx_gemm_lds" not in name:
+            continue
+        at = [i for i, s in enumerate(code) if s.startswith("v_mfma")]
+        for i in at:
+            acc = re.match(r"v_mfma_scale_f32_16x16x128_f8f6f4 (a\[\d+:\d+\]), v\[\d+:\d+\], v\[\d+:\d+\], \1,", code[i])
+            assert acc, code[i]
+        reads = [i for i, s in enumerate(code) if re.search(r"\ba\d+\b|\ba\[", s) and not s.startswith("v_mfma")
+                 and not s.startswith("v_accvgpr_write")]
+        assert reads and min(reads) > max(at)
+        between = code[max(at):min(reads)]
+        assert between.count("s_nop 15") == 2
+        # between the products nothing is read, and one set of zeros in one piece, for a tile, is all that is written
+        moves = [i for i in range(min(at), max(at)) if "accvgpr" in code[i]]
+        assert all(code[i].startswith("v_accvgpr_write") for i in moves)
+        assert not any(moves[0] < i < moves[-1] for i in at)
+        # what the vector unit writes a product reads two wait states later at the earliest
+        for i in at:
+            read = [range(int(a), int(b or a) + 1) for a, b in re.findall(r"\bv\[?(\d+)(?::(\d+)\])?", code[i])]
+            assert len(read) == 4, code[i]
+            for s in code[i - 2:i]:
+                w = re.match(r"v_(?!mfma)\S+ v\[?(\d+)(?::(\d+)\])?", s)
+                written = range(int(w.group(1)), int(w.group(2) or w.group(1)) + 1) if w else ()
+                assert not any(v in r for r in read for v in written), (s, code[i])
+                assert not s.startswith("v_accvgpr_write"), (s, code[i])
+        checked += 1
+    assert checked == 4
