@@ -111,7 +111,7 @@ def test_linear_refusals():
     assert f(w, q, rows=41) == f(w, q, rows=-1) == f(w, q, ld=511) == f(w, q, ldy=383) == f(w, _bind(40, 513, base=0x900000)) == fq.FQ_ERR_SHAPE
     assert f(q, q) == fq.FQ_ERR_SHAPE                # the space for Q(X) is W itself
     assert f(_bind(384, 512, fq.FQ_MX_COLS), q) == f(w, _bind(40, 512, fq.FQ_MX_COLS, 0x900000)) == fq.FQ_ERR_NULL
-    assert f(w, _bind(0, 512), x=None, rows=0, y=None) == fq.FQ_OK
+    assert f(w, _bind(0, 512, base=0x900000), x=None, rows=0, y=None) == fq.FQ_OK
 
 
 def test_form_says_which_tiles_run():
