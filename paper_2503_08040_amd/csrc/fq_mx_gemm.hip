@@ -471,10 +471,12 @@ int64_t tiles_of(int M, int N, int rows, int cols) {
 }
 
 // Microseconds that the tiles of 256 x 256 (one workgroup per compute unit) and of 128 x 128 (two) take, fitted to
-// measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 128 to 11008 on 256 compute units; the
+// measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 256 to 11008 on 256 compute units; the
 // model is within 15 % of them where the two are close.  A full round of 256 x 256 tiles takes 5 + 0.82 per block of the
 // contraction (power holds the clock down), a part of a round less; of 128 x 128 tiles, a quarter of that output a
-// tile, 2.5 + 0.535 per block, half a round or less 1 + 0.28.
+// tile, 2.3 + 0.52 per block, half a round or less 1 + 0.11 to 0.29.  Measured for both: 2304 x 4096 over 4096 28.0 and
+// 27.5 us, 1100 x 8192 over 8192 48.3 and 51.9, over 2048 18.8 and 18.1, 4096 x 4096 over 4096 35.6 and 41.2, 2048 x 4096
+// over 4096 28.1 and 22.0.
 double time_256(int64_t n, int nkb, int cus) {
   const int64_t full = n / cus;
   const double f = (double)(n % cus) / cus;
@@ -483,15 +485,15 @@ double time_256(int64_t n, int nkb, int cus) {
 double time_128(int64_t n, int nkb, int cus) {
   const int64_t full = n / (2 * cus);
   const double f = (double)(n % (2 * cus)) / (2 * cus);
-  return 4 + full * (2.5 + 0.535 * nkb) + (f > 0.5 ? 2.5 + 0.52 * nkb : f > 0 ? 1 + 0.28 * nkb : 0);
+  return 4 + full * (2.3 + 0.52 * nkb) + (f > 0.5 ? 1.5 + 0.5 * nkb : f > 0 ? 1 + (0.11 + 0.35 * f) * nkb : 0);
 }
 
 }  // namespace
 
 // The largest tiles of which there are more than half as many as compute units: fewer leave the chip idle, more move
 // more bytes per product.  1024 x 2048 outputs (128 tiles of 128 x 128, 512 of 64 x 64) take the same time either way,
-// 256 x 11008 (172, 688) 12.6 and 17.9 us at a contraction of 4096, 1024 x 1024 (64, 256) 10.5 and 8.1;
-// 256 x 1024 (64 tiles of 64 x 64, 256 of 32 x 32) 7.0 and 4.7.  A tile more than twice as high or wide as the output
+// 256 x 11008 (172, 688) 11.6 and 17.9 us at a contraction of 4096, 1024 x 1024 (64, 256) 10.6 and 8.4;
+// 256 x 1024 (64 tiles of 64 x 64, 256 of 32 x 32) 7.0 and 4.8.  A tile more than twice as high or wide as the output
 // is for nothing.
 MxForm mx_form(int M, int N, int nkb, int cus) {
   const int narrow = std::min(M, N);
@@ -505,8 +507,8 @@ MxForm mx_form(int M, int N, int nkb, int cus) {
 }
 
 // The forward of a linear layer quantizes X inside its product where that is the faster way.  A workgroup then reads
-// its 16 rows of X in bf16, four times their codes: 1 x 4096 -> 11008 takes 6.7 us instead of 8.9, 128 x 2048 -> 2048
-// 5.5 instead of 7.1, but 16 x 11008 -> 4096 15 instead of 11; even at 128 KiB.  With more than a workgroup per compute
+// its 16 rows of X in bf16, four times their codes: 1 x 4096 -> 11008 takes 6.7 us instead of 9.6, 128 x 2048 -> 2048
+// 5.7 instead of 6.5, but 16 x 11008 -> 4096 15.3 instead of 10.9; even at 128 KiB.  With more than a workgroup per compute
 // unit W comes that many times.  The sums are those of the stored codes' product: 8 wavefronts share a contraction.
 bool mx_linear_fused(int M, int N, int K, int cus) {
   const MxForm form = mx_form(M, N, (K + 127) / 128, cus);

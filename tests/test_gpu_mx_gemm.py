@@ -78,8 +78,9 @@ def test_products(op, M, N, K):
 # (compute units the planner is told of, M, N, K, the tiles that follow): workgroups that walk over several tiles, edges
 # in both directions, contractions of one block and of odd and even numbers of them, shorter than the ring of stages
 TILED = [(1, 512, 512, 2048, fq.FQ_MX_FORM_256x256), (2, 700, 900, 2100, fq.FQ_MX_FORM_256x256),
-         (1, 500, 1020, 1921, fq.FQ_MX_FORM_256x256), (3, 1000, 530, 1700, fq.FQ_MX_FORM_256x256),
-         (1, 1024, 1024, 100, fq.FQ_MX_FORM_256x256), (1, 1000, 1010, 300, fq.FQ_MX_FORM_256x256),
+         (1, 500, 1020, 1921, fq.FQ_MX_FORM_256x256), (3, 1000, 700, 1700, fq.FQ_MX_FORM_256x256),
+         (3, 1000, 530, 1700, fq.FQ_MX_FORM_128x128), (1, 1024, 1024, 100, fq.FQ_MX_FORM_128x128),
+         (1, 2048, 2048, 200, fq.FQ_MX_FORM_256x256), (1, 1000, 1010, 300, fq.FQ_MX_FORM_256x256),
          (256, 4090, 4096, 1000, fq.FQ_MX_FORM_256x256),
          (1, 300, 300, 100, fq.FQ_MX_FORM_128x128), (1, 129, 400, 1, fq.FQ_MX_FORM_128x128),
          (2, 400, 333, 256, fq.FQ_MX_FORM_128x128), (1, 257, 131, 300, fq.FQ_MX_FORM_128x128),

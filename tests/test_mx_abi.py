@@ -122,7 +122,8 @@ def test_form_says_which_tiles_run():
                           (64, 11008, 4096, (fq.FQ_MX_FORM_64x64, False)), (1024, 2048, 640, (fq.FQ_MX_FORM_64x64, False)),
                           (2048, 2048, 2048, (fq.FQ_MX_FORM_128x128, False)), (512, 11008, 128, (fq.FQ_MX_FORM_128x128, False)),
                           (1500, 11008, 4096, (fq.FQ_MX_FORM_128x128, False)), (4096, 11008, 4096, (fq.FQ_MX_FORM_256x256, False)),
-                          (8192, 8192, 8192, (fq.FQ_MX_FORM_256x256, False)), (3000, 3000, 2048, (fq.FQ_MX_FORM_256x256, False)),
+                          (8192, 8192, 8192, (fq.FQ_MX_FORM_256x256, False)), (3000, 3000, 4096, (fq.FQ_MX_FORM_256x256, False)),
+                          (3000, 3000, 2048, (fq.FQ_MX_FORM_128x128, False)),
                           (16, 2 ** 20, 256, (fq.FQ_MX_FORM_32x64, True)), (2 ** 20, 40, 256, (fq.FQ_MX_FORM_64x64, False)),
                           (0, 5, 5, (0, False)), (4096, 4096, 0, (fq.FQ_MX_FORM_64x64, False))]:
         assert form(M, N, K) == want, (M, N, K, form(M, N, K))
