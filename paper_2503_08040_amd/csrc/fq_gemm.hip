@@ -1086,8 +1086,6 @@ SmallTile plan_small(int M, int N, int nkb, const TilePlan& big, int cus, bool b
   return tile;
 }
 
-}  // namespace
-
 // Compute units the planner assumes: the device's, or the value of the environment variable
 // FQ_GEMM_CUS when it is set to a positive number (tuning and tests: a small value makes small
 // problems take the mixed-geometry path).
@@ -1109,6 +1107,8 @@ int planning_cus() {
   }
   return v;
 }
+
+}  // namespace
 
 void gemm_tile_plan(int nib, int njb, int cus, int out[3]) {
   const TilePlan plan = plan_columns(nib, njb, cus > 0 ? cus : planning_cus());

@@ -177,6 +177,8 @@ hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st);
 // the tiles of an M x N output over nkb blocks of 128 on that many compute units
 enum class MxForm { k32x32, k32x64, k64x64, k128x128, k256x256 };
 MxForm mx_form(int M, int N, int nkb, int cus);
+// the current device's compute units (or FQ_GEMM_CUS); -1 if they cannot be had
+int mx_compute_units();
 // whether a linear layer's forward quantizes X inside its product
 bool mx_linear_fused(int M, int N, int K, int cus);
 
@@ -200,8 +202,6 @@ void gemm_tile_plan(int nib, int njb, int cus, int out[3]);
 void gemm_path(int M, int N, int cus, bool biased, int out[4]);
 // out = {SmallTile, workgroups}: what launch_gemm launches for an A with or without residual slots.
 void gemm_form(int M, int N, int K, int cus, bool biased, bool slots, int out[2]);
-// the current device's compute units (or FQ_GEMM_CUS); -1 if they cannot be had
-int planning_cus();
 hipError_t launch_rmsnorm(const RmsParams& p, bool backward, hipStream_t st);
 hipError_t launch_glu(const GluParams& p, bool backward, hipStream_t st);
 hipError_t launch_ctx(const CtxParams& p, bool dequantize, hipStream_t st);

@@ -3,12 +3,16 @@
 // A group of 32 values shares 2^s; s comes from the exponent of the group's largest magnitude, which is an integer
 // maximum over the bf16 bits without the sign (so infinities and NaNs come out largest), and the codes from the
 // conversion instructions, which divide by a power of two and round to E2M1 to nearest even.  Both kernels stream:
-// 2 bytes an element on the bf16 side, 17/32 per side on the other.
+// 2 bytes an element on the bf16 side, 17/32 per side on the other.  Memory bounds them: 4096 x 11008 is quantized
+// along the rows in 22.6 us (5.0 TB/s), along both in 27.6 us (5.0) and read back in 25 us (4.5), where a copy of 1 GiB
+// reaches 4.7 TB/s.  Stochastic rounding is bound by the vector unit (one Philox block per 8 elements, two conversions per
+// pair and side): both sides 34.5 us.  Below a million elements a call is latency: 3.4 us for 131 x 2200.
 //
 // A wavefront has 32 rows x 128 columns, a lane 8 x 8 of them: 16 lanes read 256 bytes of a row, four lanes next to
 // each other hold a row's group, the four lanes 16 apart a column's.  So either maximum is taken in registers with
 // two exchanges, and neither side needs the elements transposed through LDS; only the finished codes pass through it,
-// to leave in 16-byte stores.
+// to leave in 16-byte stores.  (The dword writes of the codes meet in 8 of the 64 banks; in addresses exchanged so that
+// they do not, 4096 x 11008 takes the same 27.7 us.)
 #include "fq_device.h"
 #include "fq_kernels.h"
 #include "fq_mx_device.h"
