@@ -83,19 +83,48 @@ __device__ __forceinline__ void store4(const MxGemmParams& p, const v4f& v, int 
   }
 }
 
-// 32 values of a bf16 row, from column `col` on, as packed pairs; what is not there reads as 0.
+// 32 values of a bf16 row, from column `col` on, as packed pairs; of a row that is not there zeros.  A group that ends
+// behind the row's end is read as its last 32 values, so that nothing waits here; drop_read puts it right when it is used.
 __device__ __forceinline__ void load_group(const MxGemmParams& p, int row, int col, v4u (&x)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = v4u{0u, 0u, 0u, 0u};
   if (row >= p.M) return;
-  const uint16_t* const src = p.x + row * p.ld + col;
-  if (col + 32 <= p.K) {
+  const uint16_t* const src = p.x + row * p.ld;
+  if (p.K >= 32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const v4u_at2*>(src + 8 * i);
-  } else {
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const v4u_at2*>(src + min(col, p.K - 32) + 8 * i);
+  } else if (col == 0) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (col + i < p.K) x[i >> 3][(i >> 1) & 3] |= (uint32_t)src[i] << (16 * (i & 1));
+    for (int i = 0; i < 32; ++i) x[i >> 3][(i >> 1) & 3] |= (i < p.K ? (uint32_t)src[min(i, p.K - 1)] : 0u) << (16 * (i & 1));
+  }
+}
+
+// Takes away the first n values of 32 that a group does not have.
+__device__ __forceinline__ void drop_read(int n, v4u (&x)[4]) {
+  const v4u zero = {0u, 0u, 0u, 0u};
+  if (n >= 32) x[0] = x[1] = x[2] = x[3] = zero;
+  if (n & 16) {
+    x[0] = x[2];
+    x[1] = x[3];
+    x[2] = x[3] = zero;
+  }
+  if (n & 8) {
+    x[0] = x[1];
+    x[1] = x[2];
+    x[2] = x[3];
+    x[3] = zero;
+  }
+  // up to 7 values more: 2 dwords, 1 dword, half a dword
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const v4u next = i < 3 ? x[(i + 1) & 3] : zero;
+    const uint32_t w[8] = {x[i][0], x[i][1], x[i][2], x[i][3], next[0], next[1], next[2], next[3]};
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const uint32_t a = n & 4 ? w[d + 2] : w[d], b = n & 4 ? w[d + 3] : w[d + 1], c = n & 4 ? w[d + 4] : w[d + 2];
+      const uint32_t lo = n & 2 ? b : a, hi = n & 2 ? c : b;
+      x[i][d] = n & 1 ? lo >> 16 | hi << 16 : lo;
+    }
   }
 }
 
@@ -176,8 +205,12 @@ __global__ __launch_bounds__(64 * kW) void mx_gemm_split_kernel(MxGemmParams p, 
       if (kb + u * kW >= nkb) break;
       if constexpr (kFused) {
         s.sa[u] = 0;
+        const int missing = (kb + u * kW) * 128 + 32 * (lane >> 4) - (p.K - 32);
 #pragma unroll
-        for (int i = 0; i < kM; ++i) s.sa[u] |= quantize_group(s.x[u][i], p.bias, s.a[u][i]) << (8 * i);
+        for (int i = 0; i < kM; ++i) {
+          if (missing > 0 && p.K >= 32) drop_read(missing, s.x[u][i]);
+          s.sa[u] |= quantize_group(s.x[u][i], p.bias, s.a[u][i]) << (8 * i);
+        }
       }
 #pragma unroll
       for (int i = 0; i < kM; ++i)

@@ -194,6 +194,15 @@ def test_linear_is_quantize_and_multiply(M, N, K):
                 assert torch.equal(y, want)
 
 
+def test_linear_of_every_tail():
+    """A last group of 1 to 32 values, in each quarter of a block of 128: neighbours of the row do not get in."""
+    big = matrix(3, 1100, 8)
+    gu.announce("mx linear, contractions of 1 to 1056")
+    for K in [*range(1, 34), *range(64, 97), *range(127, 162), 250, 1001, 1023, *range(1025, 1057)]:
+        x, W = big[:, 7:7 + K], fq.fq_mx_quantize(matrix(20, K, K))
+        assert torch.equal(fq.fq_mx_linear(x, W), fq.fq_mx_gemm(fq.FQ_OP_NT, fq.fq_mx_quantize(x), W)), K
+
+
 def test_linear_with_non_finite_tokens():
     x, W = matrix(5, 300, 1), fq.fq_mx_quantize(matrix(64, 300, 2))
     clean = fq.fq_mx_linear(x, W)
