@@ -6,7 +6,7 @@
 // 2 bytes an element on the bf16 side, 17/32 per side on the other.  Memory bounds them: 4096 x 11008 is quantized
 // along the rows in 22.6 us (5.0 TB/s), along both in 27.6 us (5.0) and read back in 25 us (4.5), where a copy of 1 GiB
 // reaches 4.7 TB/s.  Stochastic rounding is bound by the vector unit (one Philox block per 8 elements, two conversions per
-// pair and side): both sides 34.5 us.  Below a million elements a call is latency: 3.4 us for 131 x 2200.
+// pair and side): both sides 34.5 us.  Below a million elements a call is latency: 3.1 us for 131 x 2200.
 //
 // A wavefront has 32 rows x 128 columns, a lane 8 x 8 of them: 16 lanes read 256 bytes of a row, four lanes next to
 // each other hold a row's group, the four lanes 16 apart a column's.  So either maximum is taken in registers with
@@ -46,8 +46,19 @@ __device__ __forceinline__ uint32_t bytes(uint32_t a, uint32_t b, uint32_t c, ui
 
 struct Random8 { uint32_t w[4]; };
 
+// 8 values, the first n (1 to 7) of them dropped.
+__device__ __forceinline__ v4u drop_first(const v4u& v, int n) {
+  const uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  const int s = 16 * (n & 3);
+  const uint64_t a = lo >> s | (hi << 1) << (63 - s), b = hi >> s;
+  const uint64_t l = n & 4 ? b : a, h = n & 4 ? 0 : b;
+  return v4u{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+
 // The 8 x 8 values at (row0, col0), packed pairs; what is not there reads as 0.  All loads are requested before one of
-// them is used: behind the edges a lane reads the last row, and the last 8 columns, which it shifts.
+// them is used.  Behind the edges a lane reads the last row and the last group of 8 columns.  That group may end behind
+// its row, in what follows there; of the last row, which nothing follows, the last 8 values are read instead.  What a small
+// matrix pays for edges is the fetch of their code: 300 x 1020 with every row shifted 4.4 us, so 3.4, 300 x 1024 3.0.
 __device__ __forceinline__ void load_rows(const MxQuantParams& p, int row0, int col0, v4u (&x)[8]) {
   if (p.cols < 8) {
 #pragma unroll
@@ -59,18 +70,22 @@ __device__ __forceinline__ void load_rows(const MxQuantParams& p, int row0, int 
     }
     return;
   }
-  const int col = min(col0, p.cols - 8), missing = col0 - col;
+  const int last = p.rows - 1, col = min(col0, (p.cols - 1) & ~7), col_last = min(col, p.cols - 8);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const v4u_at2*>(p.x + min(row0 + i, p.rows - 1) * p.ld + col);
-  if (missing) {
+  for (int i = 0; i < 8; ++i)
+    x[i] = *reinterpret_cast<const v4u_at2*>(p.x + min(row0 + i, last) * p.ld + (row0 + i < last ? col : col_last));
+  const int valid = p.cols - col0;
+  if (valid < 8) {
+    if (valid > 0 && row0 == (last & ~7)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (missing & 4) x[i] = v4u{x[i][2], x[i][3], 0u, 0u};
-      if (missing & 2) x[i] = v4u{x[i][1], x[i][2], x[i][3], 0u};
-      if (missing & 1)
-        x[i] = v4u{x[i][0] >> 16 | x[i][1] << 16, x[i][1] >> 16 | x[i][2] << 16, x[i][2] >> 16 | x[i][3] << 16, x[i][3] >> 16};
-      if (missing >= 8) x[i] = v4u{0u, 0u, 0u, 0u};
+      for (int i = 0; i < 8; ++i)
+        if (i == (last & 7)) x[i] = drop_first(x[i], 8 - valid);
     }
+    v4u mask;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) mask[d] = valid >= 2 * d + 2 ? 0xFFFFFFFFu : valid == 2 * d + 1 ? 0xFFFFu : 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] &= mask;
   }
   if (row0 + 8 > p.rows) {
 #pragma unroll
