@@ -148,15 +148,18 @@ __device__ __forceinline__ uint32_t quantize_group(const v4u (&x)[4], int bias, 
 // ---- small outputs: a workgroup per tile of kM x kN strips, the contraction split over its kW wavefronts -----------
 // Operands go straight from memory to registers, kU blocks of 128 at a time; the wavefronts' sums are joined through
 // LDS in a fixed order.  kFused: A is bf16 and every workgroup quantizes the rows of its tile as it goes.  Such products
-// are latency and, for few rows, the read of B: 33 x 4096 over 11008 7.7 us (3.1 TB/s), 777 x 2201 over 1544 8.4 us.
+// are latency and, for few rows, the read of B: 33 x 4096 over 11008 7.9 us (3.0 TB/s), 777 x 2201 over 1544 7.3 us.
 // Tiles of 64 x 64 gain nothing from 8 wavefronts over 4.
 template <int kM, int kN, int kW, int kU, bool kFused>
-__global__ __launch_bounds__(64 * kW) void mx_gemm_split_kernel(MxGemmParams p, int tiles_j) {
+__global__ __launch_bounds__(64 * kW) void mx_gemm_split_kernel(MxGemmParams p, int tiles_i, int tiles) {
   static_assert(4 % kM == 0 && 4 % kN == 0, "the strips of a tile share their scale dwords");
   __shared__ v4f part[kW][kM * kN][64];
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int ti = blockIdx.x / tiles_j, tj = blockIdx.x % tiles_j;
+  // An XCD takes a run of tiles down the columns, so that its L2 holds few columns' B (777 x 2201 over 1544 in 13 x 35
+  // tiles 8.65 -> 7.3 us, 131 x 1544 over 2200 in 5 x 49 4.5 -> 3.4).
+  const unsigned place = xcd_run(blockIdx.x, tiles);
+  const int tj = place / (unsigned)tiles_i, ti = place % (unsigned)tiles_i;
   const int i0 = ti * kM, j0 = tj * kN, nkb = p.b.nkb;
   // strips behind the last one repeat it: their results are not stored
   const uint8_t *ap[kM], *bp[kN];
@@ -506,7 +509,7 @@ hipError_t through_lds(const MxGemmParams& p, int cus, hipStream_t st) {
 template <int kM, int kN, int kW, int kU, bool kFused>
 hipError_t split(const MxGemmParams& p, hipStream_t st) {
   const int ti = (p.a.strips + kM - 1) / kM, tj = (p.b.strips + kN - 1) / kN;
-  hipLaunchKernelGGL((mx_gemm_split_kernel<kM, kN, kW, kU, kFused>), dim3(ti * tj), dim3(64 * kW), 0, st, p, tj);
+  hipLaunchKernelGGL((mx_gemm_split_kernel<kM, kN, kW, kU, kFused>), dim3(ti * tj), dim3(64 * kW), 0, st, p, ti, ti * tj);
   return hipGetLastError();
 }
 
