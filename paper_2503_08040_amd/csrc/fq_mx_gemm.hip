@@ -322,11 +322,15 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
   const int wr = w / G::kWC, wc = w % G::kWC;
   const int nkb = p.a.nkb, tiles = tiles_i * tiles_j;
   const uint32_t lds0 = lds_address(lds);
-  auto tile_of = [&](int b, int& i0, int& j0) {      // first strips of this workgroup's b-th tile
-    int ti, tj;
-    tile_at<4>(xcd_run(b, tiles), tiles_i, tiles_j, ti, tj);
+  // First strips of tile b: groups of 4 tile columns, walked row by row.  Everything up to the first loads is short, as a
+  // small product waits for the fetch of its code.
+  auto tile_of = [&](int b, int& i0, int& j0) {
+    const unsigned place = xcd_run(b, tiles), group = 4u * tiles_i, g = place / group, within = place - g * group;
+    const unsigned across = min(4u, tiles_j - 4 * g);
+    const unsigned by = across == 4 ? 0x40000000u : across == 3 ? 0x55555556u : 0x80000000u;
+    const unsigned ti = across == 1 ? within : __umulhi(within, by);      // within / across, exact below 2^30
     i0 = ti * G::kStrips;
-    j0 = tj * G::kStrips;
+    j0 = (4 * g + within - ti * across) * G::kStrips;
   };
 
   // The loader's side.  What this wavefront loads of a tile: kLoads strips, the first half of the wavefronts of A, the
@@ -334,16 +338,17 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
   const bool of_b = w >= G::kWaves / 2;
   const MxSide side = of_b ? p.b : p.a;
   const int8_t *strip[kLoads], *quad[kScaleLoads];
+  const unsigned row_codes = (unsigned)nkb * kOperand, row_scales = (unsigned)nkb * kScaleBlock;      // nkb < kMaxBlocks
   auto aim = [&](int b) {
     int i0, j0;
     tile_of(b, i0, j0);
     const int s0 = (of_b ? j0 : i0) + w % (G::kWaves / 2) * kLoads;
 #pragma unroll
     for (int n = 0; n < kLoads; ++n)
-      strip[n] = reinterpret_cast<const int8_t*>(side.codes) + (int64_t)min(s0 + n, side.strips - 1) * nkb * kOperand;
+      strip[n] = reinterpret_cast<const int8_t*>(side.codes) + (uint64_t)(unsigned)min(s0 + n, side.strips - 1) * row_codes;
 #pragma unroll
     for (int n = 0; n < kScaleLoads; ++n)
-      quad[n] = reinterpret_cast<const int8_t*>(side.scales) + (int64_t)min((s0 >> 2) + n, side.quads - 1) * nkb * kScaleBlock;
+      quad[n] = reinterpret_cast<const int8_t*>(side.scales) + (uint64_t)(unsigned)min((s0 >> 2) + n, side.quads - 1) * row_scales;
   };
   int aimed = blockIdx.x, ahead = 0;      // tile and block to load next
   unsigned code_off = lane * 16u, scale_off = lane * 4u;
@@ -359,12 +364,12 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
     stage_at = stage_at == lds0 + (G::kStages - 1) * G::kStage ? lds0 : stage_at + G::kStage;
     code_off += kOperand;
     scale_off += kScaleBlock;
-    if (++ahead < nkb) return;
+    if (__builtin_expect(++ahead < nkb, 1)) return;
     if (aimed + (int)gridDim.x < tiles) {
       aimed += gridDim.x;
       aim(aimed);
-      code_off -= (unsigned)nkb * kOperand;
-      scale_off -= (unsigned)nkb * kScaleBlock;
+      code_off -= row_codes;
+      scale_off -= row_scales;
       ahead = 0;
     } else {
       --ahead;
