@@ -563,27 +563,35 @@ int mx_compute_units() {
 // The largest tiles of which there are more than half as many as compute units: fewer leave the chip idle, more move
 // more bytes per product.  1024 x 2048 outputs (128 tiles of 128 x 128, 512 of 64 x 64) take the same time either way,
 // 256 x 11008 (172, 688) 11.6 and 17.9 us at a contraction of 4096, 1024 x 1024 (64, 256) 10.6 and 8.4;
-// 256 x 1024 (64 tiles of 64 x 64, 256 of 32 x 32) 7.0 and 4.8.  A tile more than twice as high or wide as the output
-// is for nothing.
+// 256 x 1024 (64 tiles of 64 x 64, 256 of 32 x 32) 7.2 and 4.9.  While two workgroups of 64 x 64 tiles per compute unit
+// hold them all and the contraction is short, those are faster where the edges waste larger ones: 300 x 6000 over 1000
+// (141, 470) 6.6 and 5.5, 777 x 2432 (133, 494) over 1544 7.2 and 7.0, but over 4096 11.1 and 11.9.  A tile more than
+// twice as high or wide as the output is for nothing.
 MxForm mx_form(int M, int N, int nkb, int cus) {
   const int narrow = std::min(M, N);
-  const int64_t n128 = tiles_of(M, N, 128, 128);
-  if (narrow > 64 && 2 * n128 > cus && nkb > 0 && nkb < kMaxBlocks)
+  const int64_t n128 = tiles_of(M, N, 128, 128), n64 = tiles_of(M, N, 64, 64);
+  const bool at_once = n64 <= 2 * cus && nkb <= 16;
+  if (narrow > 64 && 2 * n128 > cus && !at_once && nkb > 0 && nkb < kMaxBlocks)
     return narrow > 128 && time_256(tiles_of(M, N, 256, 256), nkb, cus) < time_128(n128, nkb, cus) ? MxForm::k256x256
                                                                                                    : MxForm::k128x128;
-  if (narrow > 32 && 2 * tiles_of(M, N, 64, 64) > cus) return MxForm::k64x64;
+  if (narrow > 32 && 2 * n64 > cus) return MxForm::k64x64;
   if (N > 32 && 2 * tiles_of(M, N, 32, 64) > cus) return MxForm::k32x64;
   return MxForm::k32x32;
 }
 
 // The forward of a linear layer quantizes X inside its product where that is the faster way.  A workgroup then reads
-// its 16 rows of X in bf16, four times their codes: 1 x 4096 -> 11008 takes 6.7 us instead of 9.6, 128 x 2048 -> 2048
-// 5.7 instead of 6.5, but 16 x 11008 -> 4096 15.3 instead of 10.9; even at 128 KiB.  With more than a workgroup per compute
-// unit W comes that many times.  The sums are those of the stored codes' product: 8 wavefronts share a contraction.
+// its 16 rows of X in bf16, four times their codes, and with more workgroups than compute units that is repeated:
+// 1 x 4096 -> 11008 takes 6.7 us instead of 9.6, 128 x 2048 -> 2048 (256 workgroups) 5.7 instead of 6.6, 16 x 11008 -> 4096
+// 15.3 instead of 10.9, 200 x 500 -> 2000 (416) 4.5 instead of 6.6, 200 x 2000 -> 2000 8.1 instead of 7.8,
+// 32 x 1000 -> 30000 (938) 9.9 instead of 10.4, 32 x 512 -> 60000 (1876) 14.7 instead of 13.1; 16 x 4096 -> 32000 (500) the
+// same, -> 128000 65 instead of 57.
+// The sums are those of the stored codes' product: 8 wavefronts share a contraction.
 bool mx_linear_fused(int M, int N, int K, int cus) {
   const MxForm form = mx_form(M, N, (K + 127) / 128, cus);
   if (form != MxForm::k32x32 && form != MxForm::k32x64) return false;
-  return (int64_t)std::min(M, 16) * K <= 65536 && (M <= 16 || tiles_of(M, N, 16, 64) <= cus + cus / 4);
+  const int64_t n = tiles_of(M, N, 16, 64), read = (int64_t)std::min(M, 16) * K;
+  if (M <= 16) return read <= (n <= 2 * cus ? 65536 : 32768);
+  return n <= cus ? K <= 4096 : n <= 4 * cus && K <= 1024;
 }
 
 hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st) {
