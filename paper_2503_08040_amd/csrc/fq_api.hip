@@ -622,7 +622,7 @@ fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contractio
   const int cus = compute_units > 0 ? compute_units : fq::mx_compute_units();
   if (cus <= 0) return FQ_ERR_HIP;
   form[0] = rows_out && cols_out ? (int32_t)fq::mx_form(rows_out, cols_out, (int)ceil_div(contraction, 128), cus) : 0;
-  form[1] = rows_out && cols_out ? fq::mx_linear_fused(rows_out, cols_out, contraction, cus) : 0;
+  form[1] = rows_out && cols_out ? fq::mx_linear_fused(rows_out, cols_out, contraction, cus, false) : 0;
   return FQ_OK;
 }
 
@@ -652,7 +652,8 @@ fq_status fq_mx_linear(const void* x_bf16, int32_t rows, int64_t ld, fq_mx_rule 
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int cus = fq::mx_compute_units();
   if (cus <= 0) return FQ_ERR_HIP;
-  if (q.x && (!xq || fq::mx_linear_fused(g.M, g.N, q.cols, cus))) {
+  const bool unaligned = ((uintptr_t)q.x & 3) || (rows > 1 && (ld & 1));
+  if (q.x && (!xq || fq::mx_linear_fused(g.M, g.N, q.cols, cus, unaligned))) {
     g.x = q.x; g.ld = q.ld; g.K = q.cols; g.bias = q.bias;
   } else if (q.x && fq::launch_mx_quantize(q, st) != hipSuccess) {
     return FQ_ERR_HIP;

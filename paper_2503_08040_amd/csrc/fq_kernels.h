@@ -179,8 +179,8 @@ enum class MxForm { k32x32, k32x64, k64x64, k128x128, k256x256 };
 MxForm mx_form(int M, int N, int nkb, int cus);
 // the current device's compute units (or FQ_GEMM_CUS); -1 if they cannot be had
 int mx_compute_units();
-// whether a linear layer's forward quantizes X inside its product
-bool mx_linear_fused(int M, int N, int K, int cus);
+// whether a linear layer's forward quantizes X inside its product; unaligned: X's rows do not all begin at dwords
+bool mx_linear_fused(int M, int N, int K, int cus, bool unaligned);
 
 hipError_t launch_quantize(const QuantParams& p, hipStream_t st);
 hipError_t launch_untile(const int8_t* tiled, int rows, int cols, int8_t* dense, hipStream_t st);
