@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * kW) void mx_gemm_split_kernel(MxGemmParams p, 
   }
 }
 
-// The same instruction in place and in order.  With 256 of 512 registers as accumulators the compiler's allocation of its
+// The same instruction in place and in order.  With half of the registers as accumulators the compiler's allocation of its
 // own form moves them about in the loop.  What follows a matrix instruction and reads acc other than as another's
 // accumulator has to wait by itself.
 template <int kSa, int kSb>
