@@ -29,7 +29,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 
 constexpr int kMaxDevices = 64;   // per-device host-side caches
-constexpr int kMaxBlocks = 1 << 22;   // blocks of a contraction whose codes' offsets fit 32 bits
+constexpr int kMaxBlocks = 1 << 21;   // blocks of a contraction whose codes' offsets fit 31 bits
 constexpr int kFp4 = 4;           // the instruction's format code of E2M1
 
 // acc += a b with byte kSa of sa, kSb of sb: rows of `a` go to registers, rows of `b` to lanes, so with C's columns

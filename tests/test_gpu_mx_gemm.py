@@ -289,6 +289,57 @@ def test_a_step_replays_from_a_graph():
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dw, t), want))
 
 
+@pytest.mark.parametrize("cus,M,N,K", [(256, 1100, 2000, 700), (2, 700, 900, 500)])
+def test_large_tiles_replay_from_a_graph(cus, M, N, K, monkeypatch):
+    """Tiles of 128 x 128 and 256 x 256 that walk over the output, one output of either type."""
+    monkeypatch.setenv("FQ_GEMM_CUS", str(cus))
+    tiles = fq.fq_mx_gemm_form(M, N, K)[0]
+    assert tiles == (fq.FQ_MX_FORM_256x256 if cus == 2 else fq.FQ_MX_FORM_128x128)
+    x, w = matrix(M, K, 1), matrix(N, K, 2)
+    qx, qw = fq.MxTensor(M, K), fq.MxTensor(N, K)
+    y, z = torch.empty((M, N), device="cuda"), torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        fq.fq_mx_quantize(w, out=qw)
+        fq.fq_mx_linear(x, qw, xq=qx, out=y)
+        fq.fq_mx_gemm(fq.FQ_OP_NT, qx, qw, out=z)
+
+    graph = torch.cuda.CUDAGraph()
+    gu.announce(f"capturing products in tiles {tiles}")
+    with torch.cuda.graph(graph):
+        step()
+    for rep in range(4):
+        x.copy_(matrix(M, K, 10 + rep))
+        w.copy_(matrix(N, K, 20 + rep))
+        step()
+        want = y.clone(), z.clone()
+        y.zero_(), z.zero_()
+        torch.cuda.synchronize()
+        gu.announce(f"replay {rep}")
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(z, want[1])
+
+
+def test_two_products_at_once():
+    """Products and a quantizer on three streams share nothing."""
+    A, B = pair(fq.FQ_OP_NT, 1500, 1700, 900)
+    P, Q = pair(fq.FQ_OP_TN, 2300, 4100, 400, 7)
+    x = matrix(900, 1000, 3)
+    want = fq.fq_mx_gemm(fq.FQ_OP_NT, A, B), fq.fq_mx_gemm(fq.FQ_OP_TN, P, Q), fq.fq_mx_quantize_sr(x, 9, sides=fq.FQ_MX_BOTH)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = [torch.empty_like(want[0]), torch.empty_like(want[1]), fq.MxTensor(900, 1000, fq.FQ_MX_BOTH)]
+    torch.cuda.synchronize()
+    gu.announce("three mx calls at once")
+    for _ in range(20):
+        fq.fq_mx_gemm(fq.FQ_OP_NT, A, B, out=got[0], stream=streams[0])
+        fq.fq_mx_gemm(fq.FQ_OP_TN, P, Q, out=got[1], stream=streams[1])
+        fq.fq_mx_quantize_sr(x, 9, out=got[2], stream=streams[2])
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert all(torch.equal(got[2].view(f), want[2].view(f)) for f in ("codes", "scales", "codes_t", "scales_t"))
+
+
 def test_native_calls_are_the_ctypes_calls(monkeypatch):
     """Results, errors, the current stream: the same with and without the native module."""
     pytest.importorskip("paper_2503_08040_amd._fqnative")
