@@ -5,9 +5,9 @@
 // 17/32 byte an element.  The storage order (fq.h) makes 1 KiB of codes one operand, lane by lane, and a dword of
 // scales the four operands of 64 rows, told apart by the instruction's byte select.
 //
-// Measured, bf16 outputs: 8192 x 8192 over 8192 231 us (4.8 PFLOP/s), 4096 x 4096 over 11008 81 us (4.6), 4096 x 11008
-// over 4096 92 us (4.0, the third round of tiles is two thirds full), 2048 x 2048 over 2048 9.2 us, 512 x 512 over 512
-// 2.8 us (a launch is about 2.5), one token 4096 -> 11008 6.2 us (3.9 TB/s of W).  This instruction alone does
+// Measured, bf16 outputs: 8192 x 8192 over 8192 224 to 237 us by card (4.6 to 4.9 PFLOP/s), 4096 x 4096 over 11008 79 us
+// (4.7), 4096 x 11008 over 4096 89 us (4.1, the third round of tiles is two thirds full), 2048 x 2048 over 2048 9.0 us,
+// 512 x 512 over 512 2.8 us (a launch is about 2.5), one token 4096 -> 11008 6.2 us (3.9 TB/s of W).  This instruction alone does
 // 7.3 PFLOP/s on random codes and 9.8 on zeros: power bounds the large ones.  A block of a 256 x 256 tile takes 0.54 us
 // on 64 compute units (1308 cycles at 2.4 GHz; its products are 1024) and 0.83 us on all 256.
 #include <algorithm>
