@@ -529,7 +529,8 @@ typedef enum fq_mx_form {
   FQ_MX_FORM_32x64 = 1,
   FQ_MX_FORM_64x64 = 2,
   FQ_MX_FORM_128x128 = 3,
-  FQ_MX_FORM_256x256 = 4
+  FQ_MX_FORM_128x256 = 4,
+  FQ_MX_FORM_256x256 = 5
 } fq_mx_form;
 
 /* form[0]: the tiles of fq_mx_gemm for a rows_out x cols_out output and a contraction of that length (an fq_mx_form, 0

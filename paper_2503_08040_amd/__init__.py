@@ -28,7 +28,8 @@ FQ_MX_GROUP = 32
 FQ_MX_LINEAR_ROWS = 16
 FQ_MX_ROWS, FQ_MX_COLS, FQ_MX_BOTH = 1, 2, 3
 FQ_MX_FLOOR, FQ_MX_COVER = 0, 1
-FQ_MX_FORM_32x32, FQ_MX_FORM_32x64, FQ_MX_FORM_64x64, FQ_MX_FORM_128x128, FQ_MX_FORM_256x256 = 0, 1, 2, 3, 4
+FQ_MX_FORM_32x32, FQ_MX_FORM_32x64, FQ_MX_FORM_64x64, FQ_MX_FORM_128x128 = 0, 1, 2, 3
+FQ_MX_FORM_128x256, FQ_MX_FORM_256x256 = 4, 5
 FQ_FORM_256x256, FQ_FORM_32x32, FQ_FORM_128x64, FQ_FORM_128x128, FQ_FORM_LOADERS_128x64, FQ_FORM_LOADERS_128x128, \
     FQ_FORM_LOADERS_128x256 = 0, 1, 2, 3, 4, 5, 6
 

@@ -614,7 +614,7 @@ fq_status fq_mx_gemm(fq_op op, const fq_mx_tensor* A, const fq_mx_tensor* B, voi
 
 static_assert((int)fq::MxForm::k32x32 == FQ_MX_FORM_32x32 && (int)fq::MxForm::k32x64 == FQ_MX_FORM_32x64 &&
               (int)fq::MxForm::k64x64 == FQ_MX_FORM_64x64 && (int)fq::MxForm::k128x128 == FQ_MX_FORM_128x128 &&
-              (int)fq::MxForm::k256x256 == FQ_MX_FORM_256x256);
+              (int)fq::MxForm::k128x256 == FQ_MX_FORM_128x256 && (int)fq::MxForm::k256x256 == FQ_MX_FORM_256x256);
 
 fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contraction, int32_t compute_units, int32_t form[2]) {
   if (!form) return FQ_ERR_NULL;

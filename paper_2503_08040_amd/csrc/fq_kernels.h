@@ -175,7 +175,7 @@ hipError_t launch_mx_quantize(const MxQuantParams& p, hipStream_t st);
 hipError_t launch_mx_dequantize(const MxDequantParams& p, hipStream_t st);
 hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st);
 // the tiles of an M x N output over nkb blocks of 128 on that many compute units
-enum class MxForm { k32x32, k32x64, k64x64, k128x128, k256x256 };
+enum class MxForm { k32x32, k32x64, k64x64, k128x128, k128x256, k256x256 };
 MxForm mx_form(int M, int N, int nkb, int cus);
 // the current device's compute units (or FQ_GEMM_CUS); -1 if they cannot be had
 int mx_compute_units();

@@ -268,22 +268,22 @@ __device__ __forceinline__ void mfma_in_place_select(v4f& acc, const v4i& a, con
 // global -> LDS loads.  There are kStages of them: while a block is multiplied out of registers, the next one's operands
 // are fetched from LDS and up to three more blocks are under way.  A workgroup walks over several tiles and the ring of
 // stages runs on from one to the next, so that only the first tile waits for its operands.
-// 256 x 256 takes 8 wavefronts of 128 x 64: 4 of 128 x 128 read a third less from LDS but leave one on a SIMD, 1408 cycles
-// a block instead of 1306, and twice the time for C.  128 x 128 takes two workgroups of 4; a ring of 8 stages was slower.
+// 128 x 256 takes 8 wavefronts of 64 x 64, 256 x 256 8 of 128 x 64: 4 of 128 x 128 read a third less from LDS but leave one
+// on a SIMD, 1408 cycles a block instead of 1306, and twice the time for C (2 to 3 % slower).  128 x 128 takes two
+// workgroups of 4; a ring of 8 stages was slower.
 template <int kR_, int kC_, int kWC_, int kOcc_, int kStages_>
 struct LdsGeo {
   static constexpr int kR = kR_, kC = kC_, kWC = kWC_, kOcc = kOcc_;        // strips of a wavefront; workgroups of a CU
   static constexpr int kWaves = 2 * kWC, kThreads = 64 * kWaves;
   static constexpr int kStages = kStages_;
-  static constexpr int kStrips = 2 * kR;                                    // of the tile along either axis
-  static constexpr int kLoads = kStrips * 2 / kWaves;                       // strips that a wavefront loads
-  static constexpr int kQuads = kStrips / 4, kScaleLoads = kQuads * 2 / kWaves;   // 64 rows' scales along an axis; loads of them
-  static constexpr int kCodes = kStrips * 2 * kOperand;                     // bytes of a stage
-  static constexpr int kStage = kCodes + kQuads * 2 * kScaleBlock;
+  static constexpr int kStripsI = 2 * kR, kStripsJ = kC * kWC, kStrips = kStripsI + kStripsJ;      // of the tile
+  static constexpr int kQuadsI = kStripsI / 4, kQuads = kStrips / 4;        // 64 rows' scales
+  static constexpr int kLoads = kStrips / kWaves;                           // strips that a wavefront loads, and one of the quads
+  static constexpr int kCodes = kStrips * kOperand;                         // bytes of a stage
+  static constexpr int kStage = kCodes + kQuads * kScaleBlock;
   static constexpr int kPatchRow = 128, kPatch = 16 * kPatchRow;            // a wavefront's patch for C
   static constexpr int kLds = kStages * kStage + kWaves * kPatch;
-  static_assert(kR % 4 == 0 && kC % 4 == 0 && kC * kWC == kStrips && kOcc * kLds <= 160 * 1024);
-  static_assert(kLoads * kWaves == 2 * kStrips && kScaleLoads * kWaves == 2 * kQuads && kLoads == 4 * kScaleLoads);
+  static_assert(kR % 4 == 0 && kC % 4 == 0 && kLoads * kWaves == kStrips && kQuads <= kWaves && kOcc * kLds <= 160 * 1024);
 };
 
 // 16 rows of kChunks 16-byte chunks from a patch in LDS to C at (row0, col0); chunk c of row r lies at c ^ r.
@@ -316,7 +316,7 @@ __device__ __forceinline__ void store_patch(const MxGemmParams& p, const int8_t*
 template <class G, class T>
 __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_lds_kernel(MxGemmParams p, int tiles_i, int tiles_j) {
   extern __shared__ __attribute__((aligned(1024))) int8_t lds[];
-  constexpr int kR = G::kR, kC = G::kC, kLoads = G::kLoads, kScaleLoads = G::kScaleLoads;
+  constexpr int kR = G::kR, kC = G::kC, kLoads = G::kLoads, kAllLoads = kLoads + 1;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = w / G::kWC, wc = w % G::kWC;
@@ -329,26 +329,30 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
     const unsigned across = min(4u, tiles_j - 4 * g);
     const unsigned by = across == 4 ? 0x40000000u : across == 3 ? 0x55555556u : 0x80000000u;
     const unsigned ti = across == 1 ? within : __umulhi(within, by);      // within / across, exact below 2^30
-    i0 = ti * G::kStrips;
-    j0 = (4 * g + within - ti * across) * G::kStrips;
+    i0 = ti * G::kStripsI;
+    j0 = (4 * g + within - ti * across) * G::kStripsJ;
   };
 
-  // The loader's side.  What this wavefront loads of a tile: kLoads strips, the first half of the wavefronts of A, the
-  // others of B, and kScaleLoads times 64 rows' scales; behind the end the last ones again.
-  const bool of_b = w >= G::kWaves / 2;
-  const MxSide side = of_b ? p.b : p.a;
-  const int8_t *strip[kLoads], *quad[kScaleLoads];
+  // The loader's side.  What this wavefront loads of a tile: kLoads of the strips, A's before B's, and 64 rows' scales;
+  // behind the end the last ones again.
   const unsigned row_codes = (unsigned)nkb * kOperand, row_scales = (unsigned)nkb * kScaleBlock;      // nkb < kMaxBlocks
+  const int quad_of = min(w, G::kQuads - 1);
+  const int8_t *strip[kLoads], *quad;
   auto aim = [&](int b) {
     int i0, j0;
     tile_of(b, i0, j0);
-    const int s0 = (of_b ? j0 : i0) + w % (G::kWaves / 2) * kLoads;
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n)
-      strip[n] = reinterpret_cast<const int8_t*>(side.codes) + (uint64_t)(unsigned)min(s0 + n, side.strips - 1) * row_codes;
-#pragma unroll
-    for (int n = 0; n < kScaleLoads; ++n)
-      quad[n] = reinterpret_cast<const int8_t*>(side.scales) + (uint64_t)(unsigned)min((s0 >> 2) + n, side.quads - 1) * row_scales;
+    for (int n = 0; n < kLoads; ++n) {
+      const int s = w * kLoads + n;
+      const bool of_b = G::kStripsI % kLoads == 0 ? w >= G::kStripsI / kLoads : s >= G::kStripsI;
+      const MxSide& side = of_b ? p.b : p.a;
+      strip[n] = reinterpret_cast<const int8_t*>(side.codes) +
+                 (uint64_t)(unsigned)min(s + (of_b ? j0 - G::kStripsI : i0), side.strips - 1) * row_codes;
+    }
+    const bool of_b = quad_of >= G::kQuadsI;
+    const MxSide& side = of_b ? p.b : p.a;
+    quad = reinterpret_cast<const int8_t*>(side.scales) +
+           (uint64_t)(unsigned)min(quad_of + ((of_b ? j0 - G::kStripsI : i0) >> 2), side.quads - 1) * row_scales;
   };
   int aimed = blockIdx.x, ahead = 0;      // tile and block to load next
   unsigned code_off = lane * 16u, scale_off = lane * 4u;
@@ -356,9 +360,8 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
   aim(aimed);
   auto load = [&](int n) {
     if (n < kLoads) load_lds_at(strip[n], code_off, stage_at + (w * kLoads + n) * kOperand);
-    else load_lds_dword(quad[n - kLoads], scale_off, stage_at + G::kCodes + (w * kScaleLoads + n - kLoads) * kScaleBlock);
+    else load_lds_dword(quad, scale_off, stage_at + G::kCodes + quad_of * kScaleBlock);
   };
-  constexpr int kAllLoads = kLoads + kScaleLoads;
   // the block behind: of the next tile, or behind the last tile the last block again, into a stage that nobody reads
   auto advance = [&]() {
     stage_at = stage_at == lds0 + (G::kStages - 1) * G::kStage ? lds0 : stage_at + G::kStage;
@@ -390,9 +393,9 @@ __global__ __launch_bounds__(G::kThreads, G::kOcc * G::kWaves / 4) void mx_gemm_
     v4i a[kR], b[kC];
     int sa[kR / 4], sb[kC / 4];
   } f[2];
-  const int aoff = wr * kR * kOperand + lane * 16, boff = (G::kStrips + wc * kC) * kOperand + lane * 16;
+  const int aoff = wr * kR * kOperand + lane * 16, boff = (G::kStripsI + wc * kC) * kOperand + lane * 16;
   const int saoff = G::kCodes + wr * (kR / 4) * kScaleBlock + lane * 4;
-  const int sboff = G::kCodes + (G::kQuads + wc * (kC / 4)) * kScaleBlock + lane * 4;
+  const int sboff = G::kCodes + (G::kQuadsI + wc * (kC / 4)) * kScaleBlock + lane * 4;
   const int8_t* rd = lds;      // stage of the operands to fetch
   // A block's fetches and a stage's loads, spread over the products of a block.  With few of them the loads go first, as
   // early as their stage is free: 2048 x 2048 over 4096 in tiles of 128 x 128 14.0 -> 13.2 us (tiles of 256 x 256: no
@@ -502,7 +505,7 @@ hipError_t through_lds(const MxGemmParams& p, int cus, hipStream_t st) {
     if (e != hipSuccess) return e;
     attr_set[dev].store(true, std::memory_order_release);
   }
-  const int ti = (p.a.strips + G::kStrips - 1) / G::kStrips, tj = (p.b.strips + G::kStrips - 1) / G::kStrips;
+  const int ti = (p.a.strips + G::kStripsI - 1) / G::kStripsI, tj = (p.b.strips + G::kStripsJ - 1) / G::kStripsJ;
   const int grid = std::min(ti * tj, G::kOcc * cus);
   hipLaunchKernelGGL((mx_gemm_lds_kernel<G, T>), dim3(grid), dim3(G::kThreads), G::kLds, st, p, ti, tj);
   return hipGetLastError();
@@ -524,17 +527,23 @@ int64_t tiles_of(int M, int N, int rows, int cols) {
   return (int64_t)((M + rows - 1) / rows) * ((N + cols - 1) / cols);
 }
 
-// Microseconds that the tiles of 256 x 256 (one workgroup per compute unit) and of 128 x 128 (two) take, fitted to
-// measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 256 to 11008 on 256 compute units; the
+// Microseconds that the tiles of 256 x 256 (one workgroup per compute unit), of 128 x 256 (one) and of 128 x 128 (two)
+// take, fitted to measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 256 to 11008 on 256 compute units; the
 // model is within 15 % of them where the two are close.  A full round of 256 x 256 tiles takes 5 + 0.82 per block of the
 // contraction (power holds the clock down), a part of a round less; of 128 x 128 tiles, a quarter of that output a
-// tile, 2.3 + 0.52 per block, half a round or less 1 + 0.11 to 0.29.  Measured for both: 2304 x 4096 over 4096 28.0 and
-// 27.5 us, 1100 x 8192 over 8192 48.3 and 51.9, over 2048 18.8 and 18.1, 4096 x 4096 over 4096 35.6 and 41.2, 2048 x 4096
-// over 4096 28.1 and 22.0.
+// tile, 2.3 + 0.52 per block, half a round or less 1 + 0.11 to 0.29; of 128 x 256 tiles, one to a compute unit, 2.7 + 0.46.
+// Measured, 128 x 128, 128 x 256 and 256 x 256: 2048 x 4096 over 4096 22.5, 21.7 and 27.7 us, over 11008 51.1, 47.1 and 59.0,
+// 2048 x 11008 over 4096 58.9, 53.2 and 55.3, 512 x 11008 19.4, 18.4 and 25.4, 4096 x 4096 38.9, 38.1 and 34.7,
+// 1024 x 4096 12.8, 16.8 and 24.1, 1100 x 8192 over 2048 17.8, 20.3 and 18.1.
 double time_256(int64_t n, int nkb, int cus) {
   const int64_t full = n / cus;
   const double f = (double)(n % cus) / cus;
   return 5 + full * (5 + 0.82 * nkb) + (f > 0 ? 2 + 3 * f + (0.52 + 0.3 * f * f) * nkb : 0);
+}
+double time_128x256(int64_t n, int nkb, int cus) {
+  const int64_t full = n / cus;
+  const double f = (double)(n % cus) / cus;
+  return 4 + full * (2.7 + 0.46 * nkb) + (f > 0 ? 1.8 + (0.28 + 0.17 * f) * nkb : 0);
 }
 double time_128(int64_t n, int nkb, int cus) {
   const int64_t full = n / (2 * cus);
@@ -573,9 +582,12 @@ MxForm mx_form(int M, int N, int nkb, int cus) {
   const int narrow = std::min(M, N);
   const int64_t n128 = tiles_of(M, N, 128, 128), n64 = tiles_of(M, N, 64, 64);
   const bool at_once = n64 <= 2 * cus && nkb <= 16;
-  if (narrow > 64 && 2 * n128 > cus && !at_once && nkb > 0 && nkb < kMaxBlocks)
-    return narrow > 128 && time_256(tiles_of(M, N, 256, 256), nkb, cus) < time_128(n128, nkb, cus) ? MxForm::k256x256
-                                                                                                   : MxForm::k128x128;
+  if (narrow > 64 && 2 * n128 > cus && !at_once && nkb > 0 && nkb < kMaxBlocks) {
+    const double t128 = time_128(n128, nkb, cus), t128x256 = time_128x256(tiles_of(M, N, 128, 256), nkb, cus);
+    const double least = N > 128 ? std::min(t128, t128x256) : t128;
+    if (narrow > 128 && time_256(tiles_of(M, N, 256, 256), nkb, cus) < least) return MxForm::k256x256;
+    return least < t128 ? MxForm::k128x256 : MxForm::k128x128;
+  }
   if (narrow > 32 && 2 * n64 > cus) return MxForm::k64x64;
   if (N > 32 && 2 * tiles_of(M, N, 32, 64) > cus) return MxForm::k32x64;
   return MxForm::k32x32;
@@ -606,6 +618,7 @@ hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st) {
     case MxForm::k32x64: return split<2, 4, 8, 2, false>(p, st);
     case MxForm::k64x64: return split<4, 4, 4, 2, false>(p, st);
     case MxForm::k128x128: return through_lds<LdsGeo<4, 4, 2, 2, 4>>(p, cus, st);
+    case MxForm::k128x256: return through_lds<LdsGeo<4, 4, 4, 1, 4>>(p, cus, st);
     case MxForm::k256x256: return through_lds<LdsGeo<8, 4, 4, 1, 4>>(p, cus, st);
   }
   return hipErrorInvalidValue;

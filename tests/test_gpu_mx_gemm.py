@@ -84,7 +84,10 @@ TILED = [(1, 512, 512, 2048, fq.FQ_MX_FORM_256x256), (2, 700, 900, 2100, fq.FQ_M
          (256, 4090, 4096, 1000, fq.FQ_MX_FORM_256x256),
          (1, 300, 300, 100, fq.FQ_MX_FORM_128x128), (1, 129, 400, 1, fq.FQ_MX_FORM_128x128),
          (2, 400, 333, 256, fq.FQ_MX_FORM_128x128), (1, 257, 131, 300, fq.FQ_MX_FORM_128x128),
-         (3, 500, 420, 513, fq.FQ_MX_FORM_128x128), (1, 140, 1000, 700, fq.FQ_MX_FORM_256x256),
+         (3, 500, 420, 513, fq.FQ_MX_FORM_128x256), (4, 500, 420, 513, fq.FQ_MX_FORM_128x128),
+         (3, 100, 500, 300, fq.FQ_MX_FORM_128x256), (5, 383, 250, 300, fq.FQ_MX_FORM_128x256),
+         (1, 641, 1001, 1500, fq.FQ_MX_FORM_128x256), (8, 250, 700, 2100, fq.FQ_MX_FORM_128x256),
+         (256, 2040, 4090, 1921, fq.FQ_MX_FORM_128x256), (1, 140, 1000, 700, fq.FQ_MX_FORM_256x256),
          (1, 70, 1000, 700, fq.FQ_MX_FORM_128x128), (8, 130, 150, 900, fq.FQ_MX_FORM_64x64),
          (4, 60, 500, 600, fq.FQ_MX_FORM_64x64), (4, 30, 500, 600, fq.FQ_MX_FORM_32x64),
          (4, 100, 60, 1200, fq.FQ_MX_FORM_32x64)]
@@ -289,12 +292,12 @@ def test_a_step_replays_from_a_graph():
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dw, t), want))
 
 
-@pytest.mark.parametrize("cus,M,N,K", [(256, 1100, 2000, 700), (2, 700, 900, 500)])
+@pytest.mark.parametrize("cus,M,N,K", [(256, 1100, 2000, 700), (3, 500, 420, 513), (2, 700, 900, 500)])
 def test_large_tiles_replay_from_a_graph(cus, M, N, K, monkeypatch):
-    """Tiles of 128 x 128 and 256 x 256 that walk over the output, one output of either type."""
+    """Tiles through LDS, one output of either type."""
     monkeypatch.setenv("FQ_GEMM_CUS", str(cus))
     tiles = fq.fq_mx_gemm_form(M, N, K)[0]
-    assert tiles == (fq.FQ_MX_FORM_256x256 if cus == 2 else fq.FQ_MX_FORM_128x128)
+    assert tiles == {256: fq.FQ_MX_FORM_128x128, 3: fq.FQ_MX_FORM_128x256, 2: fq.FQ_MX_FORM_256x256}[cus]
     x, w = matrix(M, K, 1), matrix(N, K, 2)
     qx, qw = fq.MxTensor(M, K), fq.MxTensor(N, K)
     y, z = torch.empty((M, N), device="cuda"), torch.empty((M, N), dtype=torch.bfloat16, device="cuda")

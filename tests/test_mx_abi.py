@@ -120,7 +120,8 @@ def test_form_says_which_tiles_run():
                           (256, 512, 512, (fq.FQ_MX_FORM_32x32, True)), (256, 1024, 11008, (fq.FQ_MX_FORM_32x32, False)),
                           (128, 4096, 4096, (fq.FQ_MX_FORM_32x64, False)), (1024, 1024, 4096, (fq.FQ_MX_FORM_64x64, False)),
                           (64, 11008, 4096, (fq.FQ_MX_FORM_64x64, False)), (1024, 2048, 640, (fq.FQ_MX_FORM_64x64, False)),
-                          (2048, 2048, 2048, (fq.FQ_MX_FORM_128x128, False)), (512, 11008, 128, (fq.FQ_MX_FORM_128x128, False)),
+                          (2048, 2048, 2048, (fq.FQ_MX_FORM_128x128, False)), (2048, 4096, 4096, (fq.FQ_MX_FORM_128x256, False)),
+                          (5000, 129, 4096, (fq.FQ_MX_FORM_64x64, False)), (20000, 128, 4096, (fq.FQ_MX_FORM_128x128, False)), (512, 11008, 128, (fq.FQ_MX_FORM_128x128, False)),
                           (1500, 11008, 4096, (fq.FQ_MX_FORM_128x128, False)), (4096, 11008, 4096, (fq.FQ_MX_FORM_256x256, False)),
                           (8192, 8192, 8192, (fq.FQ_MX_FORM_256x256, False)), (3000, 3000, 4096, (fq.FQ_MX_FORM_256x256, False)),
                           (3000, 3000, 2048, (fq.FQ_MX_FORM_128x128, False)),

@@ -47,7 +47,7 @@ def test_registers(assembly):
             if "mx_gemm_lds" in name:
                 assert int(vgprs) <= 256, name          # two wavefronts on a SIMD
                 seen += 1
-    assert seen == 4
+    assert seen == 6
 
 
 def test_direct_loads_keep_their_wait_states(assembly):
@@ -92,4 +92,4 @@ def test_accumulators(assembly):
                 assert not any(v in r for r in read for v in written), (s, code[i])
                 assert not s.startswith("v_accvgpr_write"), (s, code[i])
         checked += 1
-    assert checked == 4
+    assert checked == 6
