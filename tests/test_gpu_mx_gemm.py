@@ -86,7 +86,7 @@ TILED = [(1, 512, 512, 2048, fq.FQ_MX_FORM_256x256), (2, 700, 900, 2100, fq.FQ_M
          (2, 400, 333, 256, fq.FQ_MX_FORM_128x128), (1, 257, 131, 300, fq.FQ_MX_FORM_128x128),
          (3, 500, 420, 513, fq.FQ_MX_FORM_128x256), (4, 500, 420, 513, fq.FQ_MX_FORM_128x128),
          (3, 100, 500, 300, fq.FQ_MX_FORM_128x256), (5, 383, 250, 300, fq.FQ_MX_FORM_128x256),
-         (1, 641, 1001, 1500, fq.FQ_MX_FORM_128x256), (8, 250, 700, 2100, fq.FQ_MX_FORM_128x256),
+         (1, 639, 999, 1500, fq.FQ_MX_FORM_128x256), (8, 250, 700, 2100, fq.FQ_MX_FORM_128x256),
          (256, 2040, 4090, 1921, fq.FQ_MX_FORM_128x256), (1, 140, 1000, 700, fq.FQ_MX_FORM_256x256),
          (1, 70, 1000, 700, fq.FQ_MX_FORM_128x128), (8, 130, 150, 900, fq.FQ_MX_FORM_64x64),
          (4, 60, 500, 600, fq.FQ_MX_FORM_64x64), (4, 30, 500, 600, fq.FQ_MX_FORM_32x64),
