@@ -96,7 +96,7 @@ def ablation_lib(name: str) -> str:
 
 
 def build_ablations(names=None, jobs: int = 6) -> list:
-    """Compile the ablation libraries (in parallel: each is a full build of the library)."""
+    """Compile the ablation libraries, in parallel: one source of each, linked with the objects that all share."""
     from concurrent.futures import ThreadPoolExecutor
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     names = list(ABLATIONS) if names is None else list(names)
@@ -108,16 +108,20 @@ def build_ablations(names=None, jobs: int = 6) -> list:
         if r.returncode != 0:
             raise RuntimeError(f"hipcc failed ({name}):\n{r.stderr}")
 
+    compile_only = [f for f in flags if f != "-shared"] + ["-c"]
+
+    # hipcc takes what follows a .hip file on its command line for source too, so objects are linked in a call of their own
     def one(name, objects):
-        run(flags + ABLATIONS[name] + ["-o", ablation_lib(name), os.path.join(CSRC, ABLATED)] + objects, name)
+        own = os.path.join(os.path.dirname(objects[0]), name + ".o")
+        run(compile_only + ABLATIONS[name] + ["-o", own, os.path.join(CSRC, ABLATED)], name)
+        run(flags + ["-o", ablation_lib(name), own] + objects, name)
         return ablation_lib(name)
 
     # the sources without switches are the same in all of them
     with ThreadPoolExecutor(max_workers=max(1, jobs)) as ex, tempfile.TemporaryDirectory() as tmp:
         common = [f for f in SOURCES if f != ABLATED]
         objects = [os.path.join(tmp, f + ".o") for f in common]
-        compile_only = [f for f in flags if f != "-shared"]
-        list(ex.map(lambda f, o: run(compile_only + ["-c", "-o", o, os.path.join(CSRC, f)], f), common, objects))
+        list(ex.map(lambda f, o: run(compile_only + ["-o", o, os.path.join(CSRC, f)], f), common, objects))
         return list(ex.map(lambda name: one(name, objects), names))
 
 
