@@ -8,6 +8,7 @@ current stream; every step of the path runs in the library's HIP kernels.  If
 the compiled library is missing, calling this package's functions raises --
 there is no fallback; without _fqnative every call goes through ctypes.
 """
+import contextlib
 import ctypes as C
 import os
 
@@ -251,6 +252,23 @@ def _stream_ptr(stream):
     if stream is not None:
         return stream.cuda_stream
     return (_current_stream or _stream_lookup())()
+
+
+# A stream that the caller gives is made the current one for the call.  What the call allocates then comes from that
+# stream's blocks: the allocator may hand out a block of another stream while its last use there is still queued, and
+# nothing would order this stream behind it.  A stream of another device makes that the current device, whose compute units
+# and functions the library asks for.
+_no_context = contextlib.nullcontext()
+
+
+def _under(stream):
+    return _no_context if stream is None else _t().cuda.stream(stream)
+
+
+def _hand_out(t, stream):
+    """t, allocated under `stream`, is not given to it again before what the caller's stream does with it by then is done."""
+    if stream is not None and t.is_cuda:
+        t.record_stream(_t().cuda.current_stream(t.device))
 
 
 def _bf16_matrix(x):
@@ -653,10 +671,14 @@ def fq_mx_quantize(x, out: MxTensor = None, sides=FQ_MX_ROWS, rule=FQ_MX_FLOOR, 
                 raise FqError(status, "fq_mx_quantize")
             return out
     rows, cols, ld = _bf16_matrix(x)
-    if out is None:
-        out = MxTensor(rows, cols, sides, x.device)
-    st = _mx_stream(stream, x, out.storage)
-    _check((_lib or lib()).fq_mx_quantize(x.data_ptr(), rows, cols, ld, int(rule), out._ref, st), "fq_mx_quantize")
+    made = out is None
+    with _under(stream):
+        if made:
+            out = MxTensor(rows, cols, sides, x.device)
+        st = _mx_stream(stream, x, out.storage)
+        _check((_lib or lib()).fq_mx_quantize(x.data_ptr(), rows, cols, ld, int(rule), out._ref, st), "fq_mx_quantize")
+    if made:
+        _hand_out(out.storage, stream)
     return out
 
 
@@ -669,11 +691,15 @@ def fq_mx_quantize_sr(x, seed, out: MxTensor = None, sides=FQ_MX_ROWS, stream=No
                 raise FqError(status, "fq_mx_quantize_sr")
             return out
     rows, cols, ld = _bf16_matrix(x)
-    if out is None:
-        out = MxTensor(rows, cols, sides, x.device)
-    st = _mx_stream(stream, x, out.storage)
-    _check((_lib or lib()).fq_mx_quantize_sr(x.data_ptr(), rows, cols, ld, C.c_uint64(seed), out._ref, st),
-           "fq_mx_quantize_sr")
+    made = out is None
+    with _under(stream):
+        if made:
+            out = MxTensor(rows, cols, sides, x.device)
+        st = _mx_stream(stream, x, out.storage)
+        _check((_lib or lib()).fq_mx_quantize_sr(x.data_ptr(), rows, cols, ld, C.c_uint64(seed), out._ref, st),
+               "fq_mx_quantize_sr")
+    if made:
+        _hand_out(out.storage, stream)
     return out
 
 
@@ -694,9 +720,13 @@ def fq_mx_dequantize(t: MxTensor, side=FQ_MX_ROWS, out=None, out_dtype=None, str
             if r[0]:
                 raise FqError(r[0], "fq_mx_dequantize")
             return r[1]
-    out, odt, ldo = _output(out, (t.rows, t.cols), out_dtype or _t().bfloat16, t.storage.device)
-    st = _mx_stream(stream, t.storage, out)
-    _check((_lib or lib()).fq_mx_dequantize(t._ref, int(side), out.data_ptr(), odt, ldo, st), "fq_mx_dequantize")
+    made = out is None
+    with _under(stream):
+        out, odt, ldo = _output(out, (t.rows, t.cols), out_dtype or _t().bfloat16, t.storage.device)
+        st = _mx_stream(stream, t.storage, out)
+        _check((_lib or lib()).fq_mx_dequantize(t._ref, int(side), out.data_ptr(), odt, ldo, st), "fq_mx_dequantize")
+    if made:
+        _hand_out(out, stream)
     return out
 
 
@@ -708,9 +738,13 @@ def fq_mx_gemm(op, A: MxTensor, B: MxTensor, out=None, out_dtype=None, stream=No
             if r[0]:
                 raise FqError(r[0], "fq_mx_gemm")
             return r[1]
-    out, cdt, ldc = _output(out, gemm_out_shape(op, A, B), out_dtype or _t().float32, A.storage.device)
-    st = _mx_stream(stream, A.storage, B.storage, out)
-    _check((_lib or lib()).fq_mx_gemm(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, st), "fq_mx_gemm")
+    made = out is None
+    with _under(stream):
+        out, cdt, ldc = _output(out, gemm_out_shape(op, A, B), out_dtype or _t().float32, A.storage.device)
+        st = _mx_stream(stream, A.storage, B.storage, out)
+        _check((_lib or lib()).fq_mx_gemm(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, st), "fq_mx_gemm")
+    if made:
+        _hand_out(out, stream)
     return out
 
 
@@ -734,12 +768,16 @@ def fq_mx_linear(x, W: MxTensor, xq: MxTensor = None, rule=FQ_MX_FLOOR, out=None
     rows, cols, ld = _bf16_matrix(x)
     if cols != W.cols:
         raise FqError(FQ_ERR_SHAPE, "fq_mx_linear")
-    if xq is None and rows > FQ_MX_LINEAR_ROWS:
-        xq = MxTensor(rows, cols, FQ_MX_ROWS, x.device)
-        if stream is not None:
-            xq.storage.record_stream(stream)        # its memory is given back when this returns
-    out, ydt, ldy = _output(out, (rows, W.rows), out_dtype or _t().float32, x.device)
-    st = _mx_stream(stream, x, W.storage, out, *([xq.storage] if xq else []))
-    _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref if xq else None, out.data_ptr(),
-                                        ydt, ldy, st), "fq_mx_linear")
+    made = out is None
+    with _under(stream):
+        if xq is None and rows > FQ_MX_LINEAR_ROWS:
+            xq = MxTensor(rows, cols, FQ_MX_ROWS, x.device)
+            if stream is not None:
+                xq.storage.record_stream(stream)    # given back when this returns; says nothing new if it is the stream's
+        out, ydt, ldy = _output(out, (rows, W.rows), out_dtype or _t().float32, x.device)
+        st = _mx_stream(stream, x, W.storage, out, *([xq.storage] if xq else []))
+        _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref if xq else None,
+                                            out.data_ptr(), ydt, ldy, st), "fq_mx_linear")
+    if made:
+        _hand_out(out, stream)
     return out
