@@ -353,10 +353,14 @@ def fq_quantize(x, crit, theta, out: QTensor = None, capacity=None, want_transpo
                 raise FqError(status, "fq_quantize")
             return out
     rows, cols, ld = _bf16_matrix(x)
-    if out is None:
-        out = QTensor(rows, cols, capacity, want_transposed, x.device, block=block)
-    _check((_lib or lib()).fq_quantize(x.data_ptr(), rows, cols, ld, out.block, int(crit), C.c_float(theta),
-                                       out._ref, _stream_ptr(stream)), "fq_quantize")
+    made = out is None
+    with _under(stream):
+        if made:
+            out = QTensor(rows, cols, capacity, want_transposed, x.device, block=block)
+        _check((_lib or lib()).fq_quantize(x.data_ptr(), rows, cols, ld, out.block, int(crit), C.c_float(theta),
+                                           out._ref, _stream_ptr(stream)), "fq_quantize")
+    if made:
+        _hand_out(out.storage, stream)
     return out
 
 
@@ -369,10 +373,14 @@ def fq_quantize_sr(x, seed, out: QTensor = None, want_transposed=False, stream=N
                 raise FqError(status, "fq_quantize_sr")
             return out
     rows, cols, ld = _bf16_matrix(x)
-    if out is None:
-        out = QTensor(rows, cols, 0, want_transposed, x.device)
-    _check((_lib or lib()).fq_quantize_sr(x.data_ptr(), rows, cols, ld, FQ_BLOCK, C.c_uint64(seed), out._ref,
-                                          _stream_ptr(stream)), "fq_quantize_sr")
+    made = out is None
+    with _under(stream):
+        if made:
+            out = QTensor(rows, cols, 0, want_transposed, x.device)
+        _check((_lib or lib()).fq_quantize_sr(x.data_ptr(), rows, cols, ld, FQ_BLOCK, C.c_uint64(seed), out._ref,
+                                              _stream_ptr(stream)), "fq_quantize_sr")
+    if made:
+        _hand_out(out.storage, stream)
     return out
 
 
@@ -380,10 +388,14 @@ def fq_quantize_topk(x, k, out: QTensor = None, capacity=None, want_transposed=F
                      stream=None) -> QTensor:
     """As fq_quantize, with the k blocks of largest abs-max falling back (Sec. 4.4)."""
     rows, cols, ld = _bf16_matrix(x)
-    if out is None:
-        out = QTensor(rows, cols, capacity, want_transposed, x.device)
-    _check((_lib or lib()).fq_quantize_topk(x.data_ptr(), rows, cols, ld, FQ_BLOCK, int(k), out._ref,
-                                            _stream_ptr(stream)), "fq_quantize_topk")
+    made = out is None
+    with _under(stream):
+        if made:
+            out = QTensor(rows, cols, capacity, want_transposed, x.device)
+        _check((_lib or lib()).fq_quantize_topk(x.data_ptr(), rows, cols, ld, FQ_BLOCK, int(k), out._ref,
+                                                _stream_ptr(stream)), "fq_quantize_topk")
+    if made:
+        _hand_out(out.storage, stream)
     return out
 
 
@@ -423,42 +435,51 @@ def fq_gemm(op, A: QTensor, B: QTensor, out=None, out_dtype=None, stream=None, _
             return r[1]
     torch = _t()
     Mo, No = gemm_out_shape(op, A, B)
-    if out is None:
-        out = torch.empty((Mo, No), dtype=out_dtype or torch.float32, device=A.storage.device)
-        ldc = max(No, 1)
-    else:
-        assert out.shape == (Mo, No) and (out.stride(1) == 1 or No <= 1)
-        ldc = out.stride(0) if Mo > 1 else max(No, 1)
-    cdt = {torch.float32: FQ_OUT_F32, torch.bfloat16: FQ_OUT_BF16}[out.dtype]
-    _check(getattr(_lib or lib(), _entry)(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, _stream_ptr(stream)),
-           _entry)
+    made = out is None
+    with _under(stream):
+        if made:
+            out = torch.empty((Mo, No), dtype=out_dtype or torch.float32, device=A.storage.device)
+            ldc = max(No, 1)
+        else:
+            assert out.shape == (Mo, No) and (out.stride(1) == 1 or No <= 1)
+            ldc = out.stride(0) if Mo > 1 else max(No, 1)
+        cdt = {torch.float32: FQ_OUT_F32, torch.bfloat16: FQ_OUT_BF16}[out.dtype]
+        _check(getattr(_lib or lib(), _entry)(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, _stream_ptr(stream)),
+               _entry)
+    if made:
+        _hand_out(out, stream)
     return out
 
 
 def fq_gemm_debug_partials(op, A: QTensor, B: QTensor, k_block, residual_term, stream=None):
     torch = _t()
     Mo, No = gemm_out_shape(op, A, B)
-    out = torch.zeros((Mo, No), dtype=torch.int32, device=A.storage.device)
-    _check(lib().fq_gemm_debug_partials(int(op), A._ref, B._ref, int(k_block),
-                                        int(bool(residual_term)), out.data_ptr(),
-                                        _stream_ptr(stream)), "fq_gemm_debug_partials")
+    with _under(stream):
+        out = torch.zeros((Mo, No), dtype=torch.int32, device=A.storage.device)
+        _check(lib().fq_gemm_debug_partials(int(op), A._ref, B._ref, int(k_block),
+                                            int(bool(residual_term)), out.data_ptr(),
+                                            _stream_ptr(stream)), "fq_gemm_debug_partials")
+    _hand_out(out, stream)
     return out
 
 
 def fq_codes_to_rowmajor(tiled, rows, cols, stream=None):
     """tiled: int8 CUDA tensor in tile order (a QTensor 'codes' view)."""
     torch = _t()
-    dense = torch.empty((rows, cols), dtype=torch.int8, device=tiled.device)
-    _check(lib().fq_codes_to_rowmajor(tiled.data_ptr(), rows, cols,
-                                      dense.data_ptr(), _stream_ptr(stream)),
-           "fq_codes_to_rowmajor")
+    with _under(stream):
+        dense = torch.empty((rows, cols), dtype=torch.int8, device=tiled.device)
+        _check(lib().fq_codes_to_rowmajor(tiled.data_ptr(), rows, cols,
+                                          dense.data_ptr(), _stream_ptr(stream)),
+               "fq_codes_to_rowmajor")
+    _hand_out(dense, stream)
     return dense
 
 
 def fq_qtensor_check(t: QTensor, stream=None) -> int:
     """Synchronizes; returns the number of flagged blocks, raises on capacity overflow."""
     n = C.c_int32(0)
-    _check(lib().fq_qtensor_check(t._ref, C.byref(n), _stream_ptr(stream)), "fq_qtensor_check")
+    with _under(stream):
+        _check(lib().fq_qtensor_check(t._ref, C.byref(n), _stream_ptr(stream)), "fq_qtensor_check")
     return int(n.value)
 
 
@@ -476,31 +497,41 @@ def fq_ctx_quantize(x, packed=None, scales=None, stream=None):
     torch = _t()
     rows, cols, ld = _bf16_matrix(x)
     ng = -(-cols // FQ_CTX_GROUP)
-    if packed is None:
-        packed = torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x.device)
-    if scales is None:
-        scales = torch.empty((rows, ng), dtype=torch.float32, device=x.device)
-    assert packed.is_contiguous() and packed.numel() == fq_ctx_packed_bytes(rows, cols)
-    assert scales.is_contiguous() and scales.numel() * 4 == fq_ctx_scales_bytes(rows, cols)
-    _check(lib().fq_ctx_quantize(x.data_ptr(), rows, cols, ld,
-                                 packed.data_ptr(), scales.data_ptr(),
-                                 _stream_ptr(stream)), "fq_ctx_quantize")
+    made = []
+    with _under(stream):
+        if packed is None:
+            packed = torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x.device)
+            made.append(packed)
+        if scales is None:
+            scales = torch.empty((rows, ng), dtype=torch.float32, device=x.device)
+            made.append(scales)
+        assert packed.is_contiguous() and packed.numel() == fq_ctx_packed_bytes(rows, cols)
+        assert scales.is_contiguous() and scales.numel() * 4 == fq_ctx_scales_bytes(rows, cols)
+        _check(lib().fq_ctx_quantize(x.data_ptr(), rows, cols, ld,
+                                     packed.data_ptr(), scales.data_ptr(),
+                                     _stream_ptr(stream)), "fq_ctx_quantize")
+    for t in made:
+        _hand_out(t, stream)
     return packed, scales
 
 
 def fq_ctx_dequantize(packed, scales, rows, cols, out=None, stream=None):
     """Inverse of fq_ctx_quantize: a bf16 [rows, cols] CUDA tensor."""
     torch = _t()
-    if out is None:
-        out = torch.empty((rows, cols), dtype=torch.bfloat16, device=packed.device)
-    assert out.dtype == torch.bfloat16 and out.shape == (rows, cols)
-    assert out.stride(1) == 1 or cols <= 1
-    assert packed.is_contiguous() and packed.numel() == fq_ctx_packed_bytes(rows, cols)
-    assert scales.is_contiguous() and scales.numel() * 4 == fq_ctx_scales_bytes(rows, cols)
-    ldo = out.stride(0) if rows > 1 else max(cols, 1)
-    _check(lib().fq_ctx_dequantize(packed.data_ptr(), scales.data_ptr(),
-                                   rows, cols, out.data_ptr(), ldo,
-                                   _stream_ptr(stream)), "fq_ctx_dequantize")
+    made = out is None
+    with _under(stream):
+        if made:
+            out = torch.empty((rows, cols), dtype=torch.bfloat16, device=packed.device)
+        assert out.dtype == torch.bfloat16 and out.shape == (rows, cols)
+        assert out.stride(1) == 1 or cols <= 1
+        assert packed.is_contiguous() and packed.numel() == fq_ctx_packed_bytes(rows, cols)
+        assert scales.is_contiguous() and scales.numel() * 4 == fq_ctx_scales_bytes(rows, cols)
+        ldo = out.stride(0) if rows > 1 else max(cols, 1)
+        _check(lib().fq_ctx_dequantize(packed.data_ptr(), scales.data_ptr(),
+                                       rows, cols, out.data_ptr(), ldo,
+                                       _stream_ptr(stream)), "fq_ctx_dequantize")
+    if made:
+        _hand_out(out, stream)
     return out
 
 
@@ -543,14 +574,17 @@ def fq_glu_forward(x1, x2, stream=None):
     assert _pitch(x1) == _pitch(x2)
     rows, cols = x1.shape
     ng = -(-cols // FQ_CTX_GROUP)
-    y = torch.empty((rows, cols), dtype=torch.bfloat16, device=x1.device)
-    ctx = [(torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x1.device),
-            torch.empty((rows, ng), dtype=torch.float32, device=x1.device)) for _ in range(2)]
-    _check(lib().fq_glu_forward(x1.data_ptr(), x2.data_ptr(), rows, cols,
-                                _pitch(x1), y.data_ptr(), _pitch(y),
-                                ctx[0][0].data_ptr(), ctx[0][1].data_ptr(),
-                                ctx[1][0].data_ptr(), ctx[1][1].data_ptr(),
-                                _stream_ptr(stream)), "fq_glu_forward")
+    with _under(stream):
+        y = torch.empty((rows, cols), dtype=torch.bfloat16, device=x1.device)
+        ctx = [(torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x1.device),
+                torch.empty((rows, ng), dtype=torch.float32, device=x1.device)) for _ in range(2)]
+        _check(lib().fq_glu_forward(x1.data_ptr(), x2.data_ptr(), rows, cols,
+                                    _pitch(x1), y.data_ptr(), _pitch(y),
+                                    ctx[0][0].data_ptr(), ctx[0][1].data_ptr(),
+                                    ctx[1][0].data_ptr(), ctx[1][1].data_ptr(),
+                                    _stream_ptr(stream)), "fq_glu_forward")
+    for t in (y, *ctx[0], *ctx[1]):
+        _hand_out(t, stream)
     return y, ctx[0], ctx[1]
 
 
@@ -559,13 +593,16 @@ def fq_glu_backward(dy, ctx1, ctx2, stream=None):
     torch = _t()
     assert dy.dtype == torch.bfloat16 and dy.dim() == 2
     rows, cols = dy.shape
-    dx1 = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
-    dx2 = torch.empty_like(dx1)
-    _check(lib().fq_glu_backward(dy.data_ptr(), _pitch(dy),
-                                 ctx1[0].data_ptr(), ctx1[1].data_ptr(),
-                                 ctx2[0].data_ptr(), ctx2[1].data_ptr(),
-                                 rows, cols, dx1.data_ptr(), dx2.data_ptr(),
-                                 _pitch(dx1), _stream_ptr(stream)), "fq_glu_backward")
+    with _under(stream):
+        dx1 = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
+        dx2 = torch.empty_like(dx1)
+        _check(lib().fq_glu_backward(dy.data_ptr(), _pitch(dy),
+                                     ctx1[0].data_ptr(), ctx1[1].data_ptr(),
+                                     ctx2[0].data_ptr(), ctx2[1].data_ptr(),
+                                     rows, cols, dx1.data_ptr(), dx2.data_ptr(),
+                                     _pitch(dx1), _stream_ptr(stream)), "fq_glu_backward")
+    for t in (dx1, dx2):
+        _hand_out(t, stream)
     return dx1, dx2
 
 
@@ -577,15 +614,18 @@ def fq_rmsnorm_forward(x, w, eps, stream=None):
     assert w.is_contiguous()
     rows, cols = x.shape
     ng = -(-cols // FQ_CTX_GROUP)
-    y = torch.empty((rows, cols), dtype=torch.bfloat16, device=x.device)
-    rstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
-    packed = torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x.device)
-    scales = torch.empty((rows, ng), dtype=torch.float32, device=x.device)
-    _check(lib().fq_rmsnorm_forward(x.data_ptr(), w.data_ptr(), rows, cols,
-                                    _pitch(x), C.c_float(eps), y.data_ptr(), _pitch(y),
-                                    packed.data_ptr(), scales.data_ptr(),
-                                    rstd.data_ptr(), _stream_ptr(stream)),
-           "fq_rmsnorm_forward")
+    with _under(stream):
+        y = torch.empty((rows, cols), dtype=torch.bfloat16, device=x.device)
+        rstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
+        packed = torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x.device)
+        scales = torch.empty((rows, ng), dtype=torch.float32, device=x.device)
+        _check(lib().fq_rmsnorm_forward(x.data_ptr(), w.data_ptr(), rows, cols,
+                                        _pitch(x), C.c_float(eps), y.data_ptr(), _pitch(y),
+                                        packed.data_ptr(), scales.data_ptr(),
+                                        rstd.data_ptr(), _stream_ptr(stream)),
+               "fq_rmsnorm_forward")
+    for t in (y, rstd, packed, scales):
+        _hand_out(t, stream)
     return y, rstd, (packed, scales)
 
 
@@ -593,12 +633,13 @@ def fq_rmsnorm_backward_static(dy, ctx, rstd, w, dx, dw, n_parts=64, stream=None
     """fq_rmsnorm_backward into caller-provided dx (bf16 [rows, cols]) and dw (float32 [cols])
     with the library's built-in scratch buffer: the call allocates nothing."""
     rows, cols = dy.shape
-    _check(lib().fq_rmsnorm_backward_static(dy.data_ptr(), _pitch(dy),
-                                            ctx[0].data_ptr(), ctx[1].data_ptr(),
-                                            rstd.data_ptr(), w.data_ptr(),
-                                            rows, cols, dx.data_ptr(), _pitch(dx),
-                                            dw.data_ptr(), int(n_parts), _stream_ptr(stream)),
-           "fq_rmsnorm_backward_static")
+    with _under(stream):
+        _check(lib().fq_rmsnorm_backward_static(dy.data_ptr(), _pitch(dy),
+                                                ctx[0].data_ptr(), ctx[1].data_ptr(),
+                                                rstd.data_ptr(), w.data_ptr(),
+                                                rows, cols, dx.data_ptr(), _pitch(dx),
+                                                dw.data_ptr(), int(n_parts), _stream_ptr(stream)),
+               "fq_rmsnorm_backward_static")
     return dx, dw
 
 
@@ -607,15 +648,18 @@ def fq_rmsnorm_backward(dy, ctx, rstd, w, n_parts=256, stream=None):
     torch = _t()
     assert dy.dtype == w.dtype == torch.bfloat16 and dy.dim() == 2 and w.is_contiguous()
     rows, cols = dy.shape
-    dx = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
-    dw = torch.empty((cols,), dtype=torch.float32, device=dy.device)
-    parts = torch.empty((n_parts * cols + rows,), dtype=torch.float32, device=dy.device)
-    _check(lib().fq_rmsnorm_backward(dy.data_ptr(), _pitch(dy),
-                                     ctx[0].data_ptr(), ctx[1].data_ptr(),
-                                     rstd.data_ptr(), w.data_ptr(), rows, cols,
-                                     dx.data_ptr(), _pitch(dx), dw.data_ptr(),
-                                     parts.data_ptr(), int(n_parts), _stream_ptr(stream)),
-           "fq_rmsnorm_backward")
+    with _under(stream):
+        dx = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
+        dw = torch.empty((cols,), dtype=torch.float32, device=dy.device)
+        parts = torch.empty((n_parts * cols + rows,), dtype=torch.float32, device=dy.device)
+        _check(lib().fq_rmsnorm_backward(dy.data_ptr(), _pitch(dy),
+                                         ctx[0].data_ptr(), ctx[1].data_ptr(),
+                                         rstd.data_ptr(), w.data_ptr(), rows, cols,
+                                         dx.data_ptr(), _pitch(dx), dw.data_ptr(),
+                                         parts.data_ptr(), int(n_parts), _stream_ptr(stream)),
+               "fq_rmsnorm_backward")
+    for t in (dx, dw):
+        _hand_out(t, stream)
     return dx, dw
 
 

@@ -2,6 +2,7 @@
 launch, without a GPU.  The allocator hands a block that was freed on a stream out again for that stream at once, while its
 last use there may still be running; what is allocated under one stream and written on another is therefore a race."""
 import contextlib
+import math
 import types
 
 import pytest
@@ -26,6 +27,12 @@ class Allocated:
 
     def dim(self):
         return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return math.prod(self.shape)
 
     def stride(self, d=None):
         s = (self.shape[-1], 1)
@@ -67,7 +74,7 @@ def world(monkeypatch):
         w.made.append(Allocated(shape, dtype, w.current))
         return w.made[-1]
 
-    fq.lib()
+    fq.MxTensor(1, 1, device="cpu")                     # the native module is looked for with the library itself
     monkeypatch.setattr(torch.cuda, "stream", under)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: w.current)
     monkeypatch.setattr(torch, "empty", empty)
@@ -78,15 +85,11 @@ def world(monkeypatch):
 
 
 def given(*shape, dtype=torch.bfloat16):
-    t = Allocated(shape, dtype, "the caller's")
-    t.is_contiguous, t.numel = lambda: True, lambda: shape[0]
-    return t
+    return Allocated(shape, dtype, "the caller's")
 
 
 def mx(rows, cols):
-    """An MxTensor of the caller's."""
-    t = fq.MxTensor(rows, cols, fq.FQ_MX_BOTH)
-    return t
+    return fq.MxTensor(rows, cols, fq.FQ_MX_BOTH)
 
 
 MX_CALLS = {
@@ -137,3 +140,62 @@ def test_what_the_caller_gives_stays_the_callers(world):
     fq.fq_mx_linear(given(40, 32), w, xq=q, out=y, stream=stream)
     assert world.made == [] and y.kept_for == q.storage.kept_for == []
     assert [s for _, s in world.launches] == [stream] * 3
+
+
+def _int8_calls():
+    """The other calls that allocate, by name: call(stream) -> what it returns, all of it allocated by the call."""
+    x, dy, w = given(40, 256), given(40, 256), given(256)
+    q, v = fq.QTensor(40, 256, want_transposed=True), fq.QTensor(48, 256)
+    ctx = given(40, 2, 160, dtype=torch.uint8), given(40, 2, dtype=torch.float32)
+    rstd, tiled = given(40, dtype=torch.float32), given(2, 16384, dtype=torch.int8)
+    return {
+        "quantize": lambda s: fq.fq_quantize(x, fq.FQ_CRIT_NONE, 0.0, stream=s),
+        "quantize_sr": lambda s: fq.fq_quantize_sr(x, 3, stream=s),
+        "quantize_topk": lambda s: fq.fq_quantize_topk(x, 1, stream=s),
+        "gemm": lambda s: fq.fq_gemm(fq.FQ_OP_NT, q, v, stream=s),
+        "gemm_plain": lambda s: fq.fq_gemm_plain(fq.FQ_OP_NT, q, v, stream=s),
+        "gemm_biased": lambda s: fq.fq_gemm_biased(fq.FQ_OP_NT, q, v, stream=s),
+        "gemm_debug_partials": lambda s: fq.fq_gemm_debug_partials(fq.FQ_OP_NT, q, v, 0, 0, stream=s),
+        "codes_to_rowmajor": lambda s: fq.fq_codes_to_rowmajor(tiled, 40, 256, stream=s),
+        "ctx_dequantize": lambda s: fq.fq_ctx_dequantize(*ctx, 40, 256, stream=s),
+        "glu_forward": lambda s: fq.fq_glu_forward(x, dy, stream=s),
+        "glu_backward": lambda s: fq.fq_glu_backward(dy, ctx, ctx, stream=s),
+        "rmsnorm_forward": lambda s: fq.fq_rmsnorm_forward(x, w, 1e-5, stream=s),
+        "rmsnorm_backward": lambda s: fq.fq_rmsnorm_backward(dy, ctx, rstd, w, stream=s),
+        "ctx_quantize": lambda s: fq.fq_ctx_quantize(x, stream=s),
+    }
+
+
+def _tensors(r):
+    if isinstance(r, (tuple, list)):
+        return [t for v in r for t in _tensors(v)]
+    return [returned(r)]
+
+
+INT8_CALLS = ["quantize", "quantize_sr", "quantize_topk", "gemm", "gemm_plain", "gemm_biased", "gemm_debug_partials",
+              "codes_to_rowmajor", "ctx_quantize", "ctx_dequantize", "glu_forward", "glu_backward", "rmsnorm_forward",
+              "rmsnorm_backward"]
+
+
+@pytest.mark.parametrize("name", INT8_CALLS)
+def test_memory_of_the_other_calls_is_allocated_under_their_stream(name, world):
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
+    call = _int8_calls()[name]
+    del world.made[:]
+    out = _tensors(call(stream))
+    hidden = [t for t in world.made if not any(t is o for o in out)]
+    assert world.made and all(t.under is stream for t in world.made)
+    assert len(hidden) == (1 if name == "rmsnorm_backward" else 0)      # its partial sums
+    assert [s for _, s in world.launches] == [stream] and world.current == "the caller's"
+    assert all("the caller's" in t.kept_for for t in out)
+
+
+@pytest.mark.parametrize("name", INT8_CALLS)
+def test_nothing_changes_in_the_other_calls_without_a_stream(name, world, monkeypatch):
+    monkeypatch.setattr(fq, "_native", None)
+    monkeypatch.setattr(fq, "_current_stream", lambda: 9)
+    monkeypatch.setattr(torch.cuda, "stream", None)
+    call = _int8_calls()[name]
+    del world.made[:]
+    out = _tensors(call(None))
+    assert all(t.under == "the caller's" and t.kept_for == [] for t in out) and len(world.launches) == 1
