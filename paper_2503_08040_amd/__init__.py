@@ -242,10 +242,10 @@ def _native_setup():
     if device and raw and same_header and _fqnative.torch_version == torch.__version__:
         _fqnative.setup(*(C.cast(f, C.c_void_p).value for f in (_native_lib.fq_quantize, _native_lib.fq_quantize_sr,
                                                                  _native_lib.fq_gemm)), device, raw)
-        _native = _fqnative
         if hasattr(_fqnative, "setup_mx"):
             names = ("quantize", "quantize_sr", "dequantize", "gemm", "linear")
             _fqnative.setup_mx(*(C.cast(getattr(_native_lib, "fq_mx_" + n), C.c_void_p).value for n in names))
+        _native = _fqnative         # at the end: another thread calls through it from here on
 
 
 def _stream_ptr(stream):
