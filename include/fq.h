@@ -535,7 +535,8 @@ typedef enum fq_mx_form {
 
 /* form[0]: the tiles of fq_mx_gemm for a rows_out x cols_out output and a contraction of that length (an fq_mx_form, 0
  * for an empty output); form[1]: 1 if fq_mx_linear computes that output in one launch when the rows of X
- * begin at 4-byte aligned addresses.  Host-only inspection, compute_units as for fq_gemm_tile_plan. */
+ * begin at 4-byte aligned addresses.  Host-only inspection, compute_units as for fq_gemm_tile_plan (more than 2^16
+ * count as 2^16).  FQ_ERR_SHAPE for negative sizes and for an output that fq_mx_gemm refuses. */
 fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contraction, int32_t compute_units,
                           int32_t form[2]);
 

@@ -484,6 +484,12 @@ bool mx_shape_ok(int32_t rows, int32_t cols) {
   return rows >= 0 && cols >= 0 && ceil_div(rows, FQ_BLOCK) * ceil_div(cols, FQ_BLOCK) <= kMxMaxBlocks;
 }
 
+// whether an M x N output is cut into as many tiles as a launch takes
+bool mx_output_ok(int32_t M, int32_t N) {
+  const int64_t i = ceil_div(M, 64), j = ceil_div(N, 64);
+  return i * j <= (i <= 1 || j <= 1 ? kMxMaxNarrow : kMxMaxBlocks);
+}
+
 // bytes of codes and scales of one side, R x C
 size_t mx_codes_bytes(int32_t R, int32_t C) { return (size_t)ceil_div(R, 16) * ceil_div(C, 128) * kMxOperandBytes; }
 size_t mx_scales_bytes(int32_t R, int32_t C) { return (size_t)ceil_div(R, 64) * ceil_div(C, 128) * kMxScaleBytes; }
@@ -536,8 +542,7 @@ fq_status prepare_mx_gemm(fq_op op, const fq_mx_tensor* A, const fq_mx_tensor* B
   if (!g->a.codes || !g->b.codes) return FQ_ERR_NULL;
   g->M = a_t ? A->cols : A->rows;
   g->N = b_t ? B->cols : B->rows;
-  const bool narrow = g->a.quads <= 1 || g->b.quads <= 1;
-  if (ldc < g->N || (int64_t)g->a.quads * g->b.quads > (narrow ? kMxMaxNarrow : kMxMaxBlocks)) return FQ_ERR_SHAPE;
+  if (ldc < g->N || !mx_output_ok(g->M, g->N)) return FQ_ERR_SHAPE;
   if (g->M == 0 || g->N == 0) return FQ_OK;
   if (!C) return FQ_ERR_NULL;
   g->c = C; g->ldc = ldc; g->out_bf16 = cdt == FQ_OUT_BF16;
@@ -618,8 +623,8 @@ static_assert((int)fq::MxForm::k32x32 == FQ_MX_FORM_32x32 && (int)fq::MxForm::k3
 
 fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contraction, int32_t compute_units, int32_t form[2]) {
   if (!form) return FQ_ERR_NULL;
-  if (rows_out < 0 || cols_out < 0 || contraction < 0) return FQ_ERR_SHAPE;
-  const int cus = compute_units > 0 ? compute_units : fq::mx_compute_units();
+  if (rows_out < 0 || cols_out < 0 || contraction < 0 || !mx_output_ok(rows_out, cols_out)) return FQ_ERR_SHAPE;
+  const int cus = compute_units > 0 ? fq::mx_plan_units(compute_units) : fq::mx_compute_units();
   if (cus <= 0) return FQ_ERR_HIP;
   form[0] = rows_out && cols_out ? (int32_t)fq::mx_form(rows_out, cols_out, (int)ceil_div(contraction, 128), cus) : 0;
   form[1] = rows_out && cols_out ? fq::mx_linear_fused(rows_out, cols_out, contraction, cus, false) : 0;

@@ -179,6 +179,9 @@ enum class MxForm { k32x32, k32x64, k64x64, k128x128, k128x256, k256x256 };
 MxForm mx_form(int M, int N, int nkb, int cus);
 // the current device's compute units (or FQ_GEMM_CUS); -1 if they cannot be had
 int mx_compute_units();
+// Units that are asked for, as the choice of tiles takes them: from 2^16 on an output of 2^23 tiles of 64 x 64 would be cut
+// into more small ones than a grid holds.
+inline int mx_plan_units(int units) { return units < 1 << 16 ? units : 1 << 16; }
 // whether a linear layer's forward quantizes X inside its product; unaligned: X's rows do not all begin at dwords
 bool mx_linear_fused(int M, int N, int K, int cus, bool unaligned);
 

@@ -523,9 +523,7 @@ hipError_t split(const MxGemmParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 
-int64_t tiles_of(int M, int N, int rows, int cols) {
-  return (int64_t)((M + rows - 1) / rows) * ((N + cols - 1) / cols);
-}
+int64_t tiles_of(int64_t M, int64_t N, int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); }
 
 // Microseconds that the tiles of 256 x 256 (one workgroup per compute unit), of 128 x 256 (one) and of 128 x 128 (two)
 // take, fitted to measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 256 to 11008 on 256 compute units; the
@@ -556,7 +554,7 @@ double time_128(int64_t n, int nkb, int cus) {
 int mx_compute_units() {
   if (const char* e = std::getenv("FQ_GEMM_CUS")) {
     const int v = std::atoi(e);
-    if (v > 0) return v;
+    if (v > 0) return mx_plan_units(v);
   }
   // per device, filled on first use (a race between threads only repeats the query)
   static std::atomic<int> cached[kMaxDevices];
