@@ -461,7 +461,7 @@ typedef enum { FQ_MX_ROWS = 1, FQ_MX_COLS = 2, FQ_MX_BOTH = 3 } fq_mx_sides;
  *   FLOOR: s = max(E - 2, -127); magnitudes beyond 6 * 2^s become 6 * 2^s (the OCP microscaling
  *     formats' rule);
  *   COVER: the smallest s >= -127 with m <= 6 * 2^s, so that nothing is cut off.
- * m = 0: byte 0 and codes 0. */
+ * m = 0: byte 0 and codes 0 with the elements' signs. */
 typedef enum { FQ_MX_FLOOR = 0, FQ_MX_COVER = 1 } fq_mx_rule;
 
 /* A microscaled matrix.  Host struct, device pointers owned by the caller; a side that is not kept
@@ -482,8 +482,8 @@ size_t fq_mx_bytes(int32_t rows, int32_t cols, int32_t sides);
 fq_status fq_mx_bind(void *base, int32_t rows, int32_t cols, int32_t sides, fq_mx_tensor *out);
 
 /*
- * Quantize x_bf16 (device, row-major [rows, ld] bf16) to the sides that `out` keeps, in one launch
- * and one read of x.  An element becomes the E2M1 value nearest to |x| / 2^s, ties to the even
+ * Quantize x_bf16 (device, row-major [rows, ld] bf16) to the sides that `out` keeps, in one launch.
+ * x is read once; for both sides of at most 128 blocks of 128 x 128, once for each.  An element becomes the E2M1 value nearest to |x| / 2^s, ties to the even
  * code, with its sign.  A group that holds an infinity or NaN gets scale byte 255 and codes 0: each
  * of its elements then stands for NaN.  With FQ_MX_COVER the magnitude that a value beyond
  * 3.5 * 2^126 rounds to is 2^128, which reads back as infinity.
@@ -514,8 +514,11 @@ fq_status fq_mx_dequantize(const fq_mx_tensor *t, int32_t side, void *out, fq_ou
 /*
  * The three products of fq_op on microscaled operands (NT reads both tensors' rows' side, NN the
  * rows' side of A and the columns' side of B, TN both columns' sides).  The products of codes and
- * scales are exact and are added in binary32, in an order that depends on the shapes only; stored
- * as binary32 or rounded once to bf16.  A group of scale byte 255 makes every output it enters NaN.
+ * scales are exact and are added in binary32, in an order that depends on the shapes and the number
+ * of compute units only (with FQ_GEMM_CUS, as for fq_gemm_tile_plan); stored as binary32 or rounded
+ * once to bf16.  What is added keeps multiples of 2^-149, so products below that vanish; a sum that
+ * passes binary32's range on the way is infinite or, where parts of both signs pass it, NaN.  A
+ * group of scale byte 255 makes every output it enters NaN.
  * C, ldc and errors as fq_gemm (FQ_ERR_NULL: also a side that the product needs and the tensor does
  * not keep); FQ_ERR_SHAPE also for an output of more than 2^23 tiles of 64 x 64, or,
  * where it has 64 rows or columns at most, of 2^21.

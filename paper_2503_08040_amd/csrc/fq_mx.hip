@@ -1,4 +1,4 @@
-// Microscaled 4-bit matrices: quantization along the rows, the columns or both from one read of x, and the way back.
+// Microscaled 4-bit matrices: quantization along the rows, the columns or both in one launch, and the way back.
 //
 // A group of 32 values shares 2^s; s comes from the exponent of the group's largest magnitude, which is an integer
 // maximum over the bf16 bits without the sign (so infinities and NaNs come out largest), and the codes from the
