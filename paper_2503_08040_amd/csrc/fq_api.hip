@@ -624,7 +624,7 @@ static_assert((int)fq::MxForm::k32x32 == FQ_MX_FORM_32x32 && (int)fq::MxForm::k3
 fq_status fq_mx_gemm_form(int32_t rows_out, int32_t cols_out, int32_t contraction, int32_t compute_units, int32_t form[2]) {
   if (!form) return FQ_ERR_NULL;
   if (rows_out < 0 || cols_out < 0 || contraction < 0 || !mx_output_ok(rows_out, cols_out)) return FQ_ERR_SHAPE;
-  const int cus = compute_units > 0 ? fq::mx_plan_units(compute_units) : fq::mx_compute_units();
+  const int cus = fq::mx_plan_units(compute_units > 0 ? compute_units : fq::compute_units());
   if (cus <= 0) return FQ_ERR_HIP;
   form[0] = rows_out && cols_out ? (int32_t)fq::mx_form(rows_out, cols_out, (int)ceil_div(contraction, 128), cus) : 0;
   form[1] = rows_out && cols_out ? fq::mx_linear_fused(rows_out, cols_out, contraction, cus, false) : 0;
@@ -655,7 +655,7 @@ fq_status fq_mx_linear(const void* x_bf16, int32_t rows, int64_t ld, fq_mx_rule 
   s = prepare_mx_quantize(x_bf16, rows, W->cols, ld, rule, &side, &q);
   if (s != FQ_OK || g.M == 0 || g.N == 0) return s;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const int cus = fq::mx_compute_units();
+  const int cus = fq::mx_plan_units(fq::compute_units());
   if (cus <= 0) return FQ_ERR_HIP;
   const bool unaligned = ((uintptr_t)q.x & 3) || (rows > 1 && (ld & 1));
   if (q.x && (!xq || fq::mx_linear_fused(g.M, g.N, q.cols, cus, unaligned))) {

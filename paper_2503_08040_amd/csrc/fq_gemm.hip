@@ -1086,32 +1086,28 @@ SmallTile plan_small(int M, int N, int nkb, const TilePlan& big, int cus, bool b
   return tile;
 }
 
-// Compute units the planner assumes: the device's, or the value of the environment variable
-// FQ_GEMM_CUS when it is set to a positive number (tuning and tests: a small value makes small
-// problems take the mixed-geometry path).
-int planning_cus() {
+}  // namespace
+
+int compute_units() {
   if (const char* e = std::getenv("FQ_GEMM_CUS")) {
     const int v = std::atoi(e);
     if (v > 0) return v;
   }
-  // per device, filled on first use (a race between threads only repeats the query)
+  // per device, filled on first use (a race between threads only repeats the query); what fails is asked again
   static std::atomic<int> cached[kMaxDevices];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return -1;
-  if (dev < 0 || dev >= kMaxDevices) dev = 0;
-  int v = cached[dev].load(std::memory_order_relaxed);
-  if (v == 0) {
-    hipDeviceProp_t prop;
-    v = hipGetDeviceProperties(&prop, dev) == hipSuccess ? prop.multiProcessorCount : -1;
-    cached[dev].store(v, std::memory_order_relaxed);
+  const bool known = dev >= 0 && dev < kMaxDevices;
+  int v = known ? cached[dev].load(std::memory_order_relaxed) : 0;
+  if (v <= 0) {
+    if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return -1;
+    if (known) cached[dev].store(v, std::memory_order_relaxed);
   }
   return v;
 }
 
-}  // namespace
-
 void gemm_tile_plan(int nib, int njb, int cus, int out[3]) {
-  const TilePlan plan = plan_columns(nib, njb, cus > 0 ? cus : planning_cus());
+  const TilePlan plan = plan_columns(nib, njb, cus > 0 ? cus : compute_units());
   out[0] = plan.n_main;
   out[1] = plan.main_tj;
   out[2] = plan.tail_tj;
@@ -1137,7 +1133,7 @@ Choice choose(int M, int N, int nkb, int cus, bool biased, bool slots) {
 void gemm_form(int M, int N, int K, int cus, bool biased, bool slots, int out[2]) {
   out[0] = out[1] = 0;
   if (M == 0 || N == 0) return;
-  const Choice c = choose(M, N, ceil_tiles(K, kBlock), cus > 0 ? cus : planning_cus(), biased, slots);
+  const Choice c = choose(M, N, ceil_tiles(K, kBlock), cus > 0 ? cus : compute_units(), biased, slots);
   constexpr int kEdges[][2] = {{0, 0}, {32, 32}, {128, 64}, {128, 128}, {128, 64}, {128, 128}, {128, 256}};
   const int* const e = kEdges[(int)c.tile];
   out[0] = (int)c.tile;
@@ -1149,7 +1145,7 @@ void gemm_path(int M, int N, int cus, bool biased, int out[4]) {
   out[0] = out[1] = out[2] = out[3] = 0;
   if (M == 0 || N == 0) return;
   constexpr int kLong = 1 << 20;      // k-blocks
-  const Choice c = choose(M, N, kLong, cus > 0 ? cus : planning_cus(), biased, true);
+  const Choice c = choose(M, N, kLong, cus > 0 ? cus : compute_units(), biased, true);
   switch (c.tile) {
     case SmallTile::kNone:
       out[1] = c.plan.n_main;
@@ -1181,7 +1177,7 @@ hipError_t launch_gemm(const GemmParams& p_in, bool debug, hipStream_t st) {
   }
   if (p_in.nib == 0 || p_in.njb == 0) return hipSuccess;
   GemmParams p = p_in;
-  const auto [plan, tile] = choose(p.M, p.N, p.nkb, planning_cus(), p.biased != 0, p.a_slot != nullptr);
+  const auto [plan, tile] = choose(p.M, p.N, p.nkb, compute_units(), p.biased != 0, p.a_slot != nullptr);
   if (tile != SmallTile::kNone) return launch_gemm_small(p, tile, st);
   p.n_main = plan.n_main;
   p.main_ti = plan.main_ti;

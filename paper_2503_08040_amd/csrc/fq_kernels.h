@@ -177,14 +177,16 @@ hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st);
 // the tiles of an M x N output over nkb blocks of 128 on that many compute units
 enum class MxForm { k32x32, k32x64, k64x64, k128x128, k128x256, k256x256 };
 MxForm mx_form(int M, int N, int nkb, int cus);
-// the current device's compute units (or FQ_GEMM_CUS); -1 if they cannot be had
-int mx_compute_units();
 // Units that are asked for, as the choice of tiles takes them: from 2^16 on an output of 2^23 tiles of 64 x 64 would be cut
 // into more small ones than a grid holds.
 inline int mx_plan_units(int units) { return units < 1 << 16 ? units : 1 << 16; }
 // whether a linear layer's forward quantizes X inside its product; unaligned: X's rows do not all begin at dwords
 bool mx_linear_fused(int M, int N, int K, int cus, bool unaligned);
 
+// Compute units that the choices of tiles assume: the current device's, or the value of the environment variable
+// FQ_GEMM_CUS when it is set to a positive number (tuning and tests: a small value makes small problems take the large
+// tiles and their edges).  -1 if they cannot be had.
+int compute_units();
 hipError_t launch_quantize(const QuantParams& p, hipStream_t st);
 hipError_t launch_untile(const int8_t* tiled, int rows, int cols, int8_t* dense, hipStream_t st);
 hipError_t launch_gemm(const GemmParams& p, bool debug, hipStream_t st);

@@ -12,7 +12,6 @@
 // on 64 compute units (1308 cycles at 2.4 GHz; its products are 1024) and 0.83 us on all 256.
 #include <algorithm>
 #include <atomic>
-#include <cstdlib>
 #include <type_traits>
 
 #include "fq_device.h"
@@ -551,24 +550,6 @@ double time_128(int64_t n, int nkb, int cus) {
 
 }  // namespace
 
-int mx_compute_units() {
-  if (const char* e = std::getenv("FQ_GEMM_CUS")) {
-    const int v = std::atoi(e);
-    if (v > 0) return mx_plan_units(v);
-  }
-  // per device, filled on first use (a race between threads only repeats the query)
-  static std::atomic<int> cached[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return -1;
-  const bool known = dev >= 0 && dev < kMaxDevices;
-  int v = known ? cached[dev].load(std::memory_order_relaxed) : 0;
-  if (v <= 0) {
-    if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return -1;
-    if (known) cached[dev].store(v, std::memory_order_relaxed);
-  }
-  return v;
-}
-
 // The largest tiles of which there are more than half as many as compute units: fewer leave the chip idle, more move
 // more bytes per product.  1024 x 2048 outputs (128 tiles of 128 x 128, 512 of 64 x 64) take the same time either way,
 // 256 x 11008 (172, 688) 11.6 and 17.9 us at a contraction of 4096, 1024 x 1024 (64, 256) 10.6 and 8.4;
@@ -609,7 +590,7 @@ bool mx_linear_fused(int M, int N, int K, int cus, bool unaligned) {
 
 hipError_t launch_mx_gemm(const MxGemmParams& p, hipStream_t st) {
   if (p.x) return split<1, 4, 8, 1, true>(p, st);
-  const int cus = mx_compute_units();
+  const int cus = mx_plan_units(compute_units());
   if (cus <= 0) return hipErrorInvalidDevice;
   switch (mx_form(p.M, p.N, p.a.nkb, cus)) {
     case MxForm::k32x32: return split<2, 2, 8, 2, false>(p, st);
