@@ -26,17 +26,35 @@ GEMM_SOURCE = os.path.join(ROOT, "paper_2503_08040_amd", "csrc", "fq_gemm.hip")
 TRAFFIC_PROFILE = os.path.join(ROOT, "profiles", "gemm_quantize_cfg2_hbm_traffic.md")
 
 
+def source_and_headers(path):
+    """A source and the headers that it includes by quoted names, each once, in the order of inclusion."""
+    import re
+    found = []
+
+    def visit(f):
+        f = os.path.normpath(f)
+        if f in found:
+            return
+        found.append(f)
+        with open(f) as src:
+            for name in re.findall(r'^\s*#include "([^"]+)"', src.read(), flags=re.M):
+                visit(os.path.join(os.path.dirname(f), name))
+
+    visit(path)
+    return found
+
+
 def measured_gemm_traffic(workload_name):
     """HBM-side bytes per fq_gemm launch as measured with rocprofv3 (FETCH_SIZE, WRITE_SIZE,
     each scaled by what the same counter reads for a copy of known size): read from the
     committed profile summary, which records the workload and the SHA-256 of the kernel source
-    it was measured on.  None when the kernel source has changed since (the figure would be
-    stale) or the summary does not cover this workload."""
+    it was measured on with the headers it includes.  None when one of them has changed since (the
+    figure would be stale) or the summary does not cover this workload."""
     import hashlib
     import re
     try:
         text = open(TRAFFIC_PROFILE).read()
-        sha = hashlib.sha256(open(GEMM_SOURCE, "rb").read()).hexdigest()
+        sha = hashlib.sha256(b"".join(open(f, "rb").read() for f in source_and_headers(GEMM_SOURCE))).hexdigest()
     except OSError:
         return None
     m = re.search(r"^gemm_traffic: workload=(\S+) bytes_per_launch=(\d+) fq_gemm_hip_sha256=([0-9a-f]{64})\s*$",
