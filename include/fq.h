@@ -20,8 +20,8 @@
  *     carried from one call to the next lives in the caller's fq_qtensor (its
  *     `epoch` field and `fb_counters` buffer).
  *     fq_qtensor structs themselves live in host memory.
- *   - Calls enqueue kernels on `hip_stream` (a hipStream_t passed as void*;
- *     NULL is the default stream) and return without waiting.
+ *   - Calls enqueue kernels on `hip_stream` (a hipStream_t of the current device
+ *     passed as void*; NULL is the default stream) and return without waiting.
  *   - Arguments are validated on the host before anything is launched; a
  *     failed validation returns a negative fq_status and launches nothing.
  *     HIP launch failures are returned as FQ_ERR_HIP.  No exception crosses

@@ -7,6 +7,10 @@ which also allocates fq_gemm's output.  PyTorch supplies device memory and the
 current stream; every step of the path runs in the library's HIP kernels.  If
 the compiled library is missing, calling this package's functions raises --
 there is no fallback; without _fqnative every call goes through ctypes.
+
+stream= (a torch.cuda.Stream; by default the current one) is the current stream, on its device, for the call: what
+the call allocates belongs to it as if allocated under torch.cuda.stream.  Ordering it after what filled the operands, and
+other streams after it, is the caller's.
 """
 import contextlib
 import ctypes as C
