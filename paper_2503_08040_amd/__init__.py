@@ -8,9 +8,8 @@ current stream; every step of the path runs in the library's HIP kernels.  If
 the compiled library is missing, calling this package's functions raises --
 there is no fallback; without _fqnative every call goes through ctypes.
 
-stream= (a torch.cuda.Stream; by default the current one) is the current stream, on its device, for the call: what
-the call allocates belongs to it as if allocated under torch.cuda.stream.  Ordering it after what filled the operands, and
-other streams after it, is the caller's.
+stream= is a torch.cuda.Stream, by default the current one.  What a call on it allocates belongs to it as if allocated under
+torch.cuda.stream.  Ordering it after what filled the operands, and other streams after it, is the caller's.
 """
 import contextlib
 import ctypes as C
@@ -258,21 +257,34 @@ def _stream_ptr(stream):
     return (_current_stream or _stream_lookup())()
 
 
-# A stream that the caller gives is made the current one for the call.  What the call allocates then comes from that
-# stream's blocks: the allocator may hand out a block of another stream while its last use there is still queued, and
-# nothing would order this stream behind it.  A stream of another device makes that the current device, whose compute units
-# and functions the library asks for.
+# What a call on a given stream allocates comes from that stream's blocks: the allocator may hand out a block of another
+# stream while its last use there is still queued, and nothing would order this stream behind it.  And the library asks the
+# current device for its compute units and functions, which has to be the stream's.  So that stream is made the current one
+# (10 us of the host with what is handed out), unless it is, or the call allocates nothing and the device is the right one.
 _no_context = contextlib.nullcontext()
+_has_device = None
 
 
-def _under(stream):
-    return _no_context if stream is None else _t().cuda.stream(stream)
+def _under(stream, allocates):
+    global _has_device
+    if stream is None:
+        return _no_context
+    torch = _t()
+    if _has_device is None:
+        _has_device = torch.cuda.is_available()
+    if _has_device and stream.device_index == torch.cuda.current_device() and \
+            (not allocates or stream.cuda_stream == _stream_ptr(None)):
+        return _no_context
+    return torch.cuda.stream(stream)
 
 
-def _hand_out(t, stream):
-    """t, allocated under `stream`, is not given to it again before what the caller's stream does with it by then is done."""
-    if stream is not None and t.is_cuda:
-        t.record_stream(_t().cuda.current_stream(t.device))
+def _hand_out(under, *tensors):
+    """Tensors allocated in `under` are not given to its stream again before what the caller's stream, the current one
+    again, does with them by then is done."""
+    if under is not _no_context:
+        for t in tensors:
+            if t.is_cuda:
+                t.record_stream(_t().cuda.current_stream(t.device))
 
 
 def _bf16_matrix(x):
@@ -358,13 +370,14 @@ def fq_quantize(x, crit, theta, out: QTensor = None, capacity=None, want_transpo
             return out
     rows, cols, ld = _bf16_matrix(x)
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         if made:
             out = QTensor(rows, cols, capacity, want_transposed, x.device, block=block)
         _check((_lib or lib()).fq_quantize(x.data_ptr(), rows, cols, ld, out.block, int(crit), C.c_float(theta),
                                            out._ref, _stream_ptr(stream)), "fq_quantize")
     if made:
-        _hand_out(out.storage, stream)
+        _hand_out(under, out.storage)
     return out
 
 
@@ -378,13 +391,14 @@ def fq_quantize_sr(x, seed, out: QTensor = None, want_transposed=False, stream=N
             return out
     rows, cols, ld = _bf16_matrix(x)
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         if made:
             out = QTensor(rows, cols, 0, want_transposed, x.device)
         _check((_lib or lib()).fq_quantize_sr(x.data_ptr(), rows, cols, ld, FQ_BLOCK, C.c_uint64(seed), out._ref,
                                               _stream_ptr(stream)), "fq_quantize_sr")
     if made:
-        _hand_out(out.storage, stream)
+        _hand_out(under, out.storage)
     return out
 
 
@@ -393,13 +407,14 @@ def fq_quantize_topk(x, k, out: QTensor = None, capacity=None, want_transposed=F
     """As fq_quantize, with the k blocks of largest abs-max falling back (Sec. 4.4)."""
     rows, cols, ld = _bf16_matrix(x)
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         if made:
             out = QTensor(rows, cols, capacity, want_transposed, x.device)
         _check((_lib or lib()).fq_quantize_topk(x.data_ptr(), rows, cols, ld, FQ_BLOCK, int(k), out._ref,
                                                 _stream_ptr(stream)), "fq_quantize_topk")
     if made:
-        _hand_out(out.storage, stream)
+        _hand_out(under, out.storage)
     return out
 
 
@@ -440,7 +455,8 @@ def fq_gemm(op, A: QTensor, B: QTensor, out=None, out_dtype=None, stream=None, _
     torch = _t()
     Mo, No = gemm_out_shape(op, A, B)
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         if made:
             out = torch.empty((Mo, No), dtype=out_dtype or torch.float32, device=A.storage.device)
             ldc = max(No, 1)
@@ -451,38 +467,40 @@ def fq_gemm(op, A: QTensor, B: QTensor, out=None, out_dtype=None, stream=None, _
         _check(getattr(_lib or lib(), _entry)(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, _stream_ptr(stream)),
                _entry)
     if made:
-        _hand_out(out, stream)
+        _hand_out(under, out)
     return out
 
 
 def fq_gemm_debug_partials(op, A: QTensor, B: QTensor, k_block, residual_term, stream=None):
     torch = _t()
     Mo, No = gemm_out_shape(op, A, B)
-    with _under(stream):
+    under = _under(stream, True)
+    with under:
         out = torch.zeros((Mo, No), dtype=torch.int32, device=A.storage.device)
         _check(lib().fq_gemm_debug_partials(int(op), A._ref, B._ref, int(k_block),
                                             int(bool(residual_term)), out.data_ptr(),
                                             _stream_ptr(stream)), "fq_gemm_debug_partials")
-    _hand_out(out, stream)
+    _hand_out(under, out)
     return out
 
 
 def fq_codes_to_rowmajor(tiled, rows, cols, stream=None):
     """tiled: int8 CUDA tensor in tile order (a QTensor 'codes' view)."""
     torch = _t()
-    with _under(stream):
+    under = _under(stream, True)
+    with under:
         dense = torch.empty((rows, cols), dtype=torch.int8, device=tiled.device)
         _check(lib().fq_codes_to_rowmajor(tiled.data_ptr(), rows, cols,
                                           dense.data_ptr(), _stream_ptr(stream)),
                "fq_codes_to_rowmajor")
-    _hand_out(dense, stream)
+    _hand_out(under, dense)
     return dense
 
 
 def fq_qtensor_check(t: QTensor, stream=None) -> int:
     """Synchronizes; returns the number of flagged blocks, raises on capacity overflow."""
     n = C.c_int32(0)
-    with _under(stream):
+    with _under(stream, False):
         _check(lib().fq_qtensor_check(t._ref, C.byref(n), _stream_ptr(stream)), "fq_qtensor_check")
     return int(n.value)
 
@@ -502,7 +520,8 @@ def fq_ctx_quantize(x, packed=None, scales=None, stream=None):
     rows, cols, ld = _bf16_matrix(x)
     ng = -(-cols // FQ_CTX_GROUP)
     made = []
-    with _under(stream):
+    under = _under(stream, packed is None or scales is None)
+    with under:
         if packed is None:
             packed = torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x.device)
             made.append(packed)
@@ -514,8 +533,7 @@ def fq_ctx_quantize(x, packed=None, scales=None, stream=None):
         _check(lib().fq_ctx_quantize(x.data_ptr(), rows, cols, ld,
                                      packed.data_ptr(), scales.data_ptr(),
                                      _stream_ptr(stream)), "fq_ctx_quantize")
-    for t in made:
-        _hand_out(t, stream)
+    _hand_out(under, *made)
     return packed, scales
 
 
@@ -523,7 +541,8 @@ def fq_ctx_dequantize(packed, scales, rows, cols, out=None, stream=None):
     """Inverse of fq_ctx_quantize: a bf16 [rows, cols] CUDA tensor."""
     torch = _t()
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         if made:
             out = torch.empty((rows, cols), dtype=torch.bfloat16, device=packed.device)
         assert out.dtype == torch.bfloat16 and out.shape == (rows, cols)
@@ -535,7 +554,7 @@ def fq_ctx_dequantize(packed, scales, rows, cols, out=None, stream=None):
                                        rows, cols, out.data_ptr(), ldo,
                                        _stream_ptr(stream)), "fq_ctx_dequantize")
     if made:
-        _hand_out(out, stream)
+        _hand_out(under, out)
     return out
 
 
@@ -578,7 +597,8 @@ def fq_glu_forward(x1, x2, stream=None):
     assert _pitch(x1) == _pitch(x2)
     rows, cols = x1.shape
     ng = -(-cols // FQ_CTX_GROUP)
-    with _under(stream):
+    under = _under(stream, True)
+    with under:
         y = torch.empty((rows, cols), dtype=torch.bfloat16, device=x1.device)
         ctx = [(torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x1.device),
                 torch.empty((rows, ng), dtype=torch.float32, device=x1.device)) for _ in range(2)]
@@ -587,8 +607,7 @@ def fq_glu_forward(x1, x2, stream=None):
                                     ctx[0][0].data_ptr(), ctx[0][1].data_ptr(),
                                     ctx[1][0].data_ptr(), ctx[1][1].data_ptr(),
                                     _stream_ptr(stream)), "fq_glu_forward")
-    for t in (y, *ctx[0], *ctx[1]):
-        _hand_out(t, stream)
+    _hand_out(under, y, *ctx[0], *ctx[1])
     return y, ctx[0], ctx[1]
 
 
@@ -597,7 +616,8 @@ def fq_glu_backward(dy, ctx1, ctx2, stream=None):
     torch = _t()
     assert dy.dtype == torch.bfloat16 and dy.dim() == 2
     rows, cols = dy.shape
-    with _under(stream):
+    under = _under(stream, True)
+    with under:
         dx1 = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
         dx2 = torch.empty_like(dx1)
         _check(lib().fq_glu_backward(dy.data_ptr(), _pitch(dy),
@@ -605,8 +625,7 @@ def fq_glu_backward(dy, ctx1, ctx2, stream=None):
                                      ctx2[0].data_ptr(), ctx2[1].data_ptr(),
                                      rows, cols, dx1.data_ptr(), dx2.data_ptr(),
                                      _pitch(dx1), _stream_ptr(stream)), "fq_glu_backward")
-    for t in (dx1, dx2):
-        _hand_out(t, stream)
+    _hand_out(under, dx1, dx2)
     return dx1, dx2
 
 
@@ -618,7 +637,8 @@ def fq_rmsnorm_forward(x, w, eps, stream=None):
     assert w.is_contiguous()
     rows, cols = x.shape
     ng = -(-cols // FQ_CTX_GROUP)
-    with _under(stream):
+    under = _under(stream, True)
+    with under:
         y = torch.empty((rows, cols), dtype=torch.bfloat16, device=x.device)
         rstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
         packed = torch.empty((rows, ng, FQ_CTX_GROUP_BYTES), dtype=torch.uint8, device=x.device)
@@ -628,8 +648,7 @@ def fq_rmsnorm_forward(x, w, eps, stream=None):
                                         packed.data_ptr(), scales.data_ptr(),
                                         rstd.data_ptr(), _stream_ptr(stream)),
                "fq_rmsnorm_forward")
-    for t in (y, rstd, packed, scales):
-        _hand_out(t, stream)
+    _hand_out(under, y, rstd, packed, scales)
     return y, rstd, (packed, scales)
 
 
@@ -637,7 +656,7 @@ def fq_rmsnorm_backward_static(dy, ctx, rstd, w, dx, dw, n_parts=64, stream=None
     """fq_rmsnorm_backward into caller-provided dx (bf16 [rows, cols]) and dw (float32 [cols])
     with the library's built-in scratch buffer: the call allocates nothing."""
     rows, cols = dy.shape
-    with _under(stream):
+    with _under(stream, False):
         _check(lib().fq_rmsnorm_backward_static(dy.data_ptr(), _pitch(dy),
                                                 ctx[0].data_ptr(), ctx[1].data_ptr(),
                                                 rstd.data_ptr(), w.data_ptr(),
@@ -652,7 +671,8 @@ def fq_rmsnorm_backward(dy, ctx, rstd, w, n_parts=256, stream=None):
     torch = _t()
     assert dy.dtype == w.dtype == torch.bfloat16 and dy.dim() == 2 and w.is_contiguous()
     rows, cols = dy.shape
-    with _under(stream):
+    under = _under(stream, True)
+    with under:
         dx = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
         dw = torch.empty((cols,), dtype=torch.float32, device=dy.device)
         parts = torch.empty((n_parts * cols + rows,), dtype=torch.float32, device=dy.device)
@@ -662,8 +682,7 @@ def fq_rmsnorm_backward(dy, ctx, rstd, w, n_parts=256, stream=None):
                                          dx.data_ptr(), _pitch(dx), dw.data_ptr(),
                                          parts.data_ptr(), int(n_parts), _stream_ptr(stream)),
                "fq_rmsnorm_backward")
-    for t in (dx, dw):
-        _hand_out(t, stream)
+    _hand_out(under, dx, dw)
     return dx, dw
 
 
@@ -720,13 +739,14 @@ def fq_mx_quantize(x, out: MxTensor = None, sides=FQ_MX_ROWS, rule=FQ_MX_FLOOR, 
             return out
     rows, cols, ld = _bf16_matrix(x)
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         if made:
             out = MxTensor(rows, cols, sides, x.device)
         st = _mx_stream(stream, x, out.storage)
         _check((_lib or lib()).fq_mx_quantize(x.data_ptr(), rows, cols, ld, int(rule), out._ref, st), "fq_mx_quantize")
     if made:
-        _hand_out(out.storage, stream)
+        _hand_out(under, out.storage)
     return out
 
 
@@ -740,14 +760,15 @@ def fq_mx_quantize_sr(x, seed, out: MxTensor = None, sides=FQ_MX_ROWS, stream=No
             return out
     rows, cols, ld = _bf16_matrix(x)
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         if made:
             out = MxTensor(rows, cols, sides, x.device)
         st = _mx_stream(stream, x, out.storage)
         _check((_lib or lib()).fq_mx_quantize_sr(x.data_ptr(), rows, cols, ld, C.c_uint64(seed), out._ref, st),
                "fq_mx_quantize_sr")
     if made:
-        _hand_out(out.storage, stream)
+        _hand_out(under, out.storage)
     return out
 
 
@@ -769,12 +790,13 @@ def fq_mx_dequantize(t: MxTensor, side=FQ_MX_ROWS, out=None, out_dtype=None, str
                 raise FqError(r[0], "fq_mx_dequantize")
             return r[1]
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         out, odt, ldo = _output(out, (t.rows, t.cols), out_dtype or _t().bfloat16, t.storage.device)
         st = _mx_stream(stream, t.storage, out)
         _check((_lib or lib()).fq_mx_dequantize(t._ref, int(side), out.data_ptr(), odt, ldo, st), "fq_mx_dequantize")
     if made:
-        _hand_out(out, stream)
+        _hand_out(under, out)
     return out
 
 
@@ -787,12 +809,13 @@ def fq_mx_gemm(op, A: MxTensor, B: MxTensor, out=None, out_dtype=None, stream=No
                 raise FqError(r[0], "fq_mx_gemm")
             return r[1]
     made = out is None
-    with _under(stream):
+    under = _under(stream, made)
+    with under:
         out, cdt, ldc = _output(out, gemm_out_shape(op, A, B), out_dtype or _t().float32, A.storage.device)
         st = _mx_stream(stream, A.storage, B.storage, out)
         _check((_lib or lib()).fq_mx_gemm(int(op), A._ref, B._ref, out.data_ptr(), cdt, ldc, st), "fq_mx_gemm")
     if made:
-        _hand_out(out, stream)
+        _hand_out(under, out)
     return out
 
 
@@ -817,7 +840,8 @@ def fq_mx_linear(x, W: MxTensor, xq: MxTensor = None, rule=FQ_MX_FLOOR, out=None
     if cols != W.cols:
         raise FqError(FQ_ERR_SHAPE, "fq_mx_linear")
     made = out is None
-    with _under(stream):
+    under = _under(stream, made or (xq is None and rows > FQ_MX_LINEAR_ROWS))
+    with under:
         if xq is None and rows > FQ_MX_LINEAR_ROWS:
             xq = MxTensor(rows, cols, FQ_MX_ROWS, x.device)
             if stream is not None:
@@ -827,5 +851,5 @@ def fq_mx_linear(x, W: MxTensor, xq: MxTensor = None, rule=FQ_MX_FLOOR, out=None
         _check((_lib or lib()).fq_mx_linear(x.data_ptr(), rows, ld, int(rule), W._ref, xq._ref if xq else None,
                                             out.data_ptr(), ydt, ldy, st), "fq_mx_linear")
     if made:
-        _hand_out(out, stream)
+        _hand_out(under, out)
     return out

@@ -199,3 +199,19 @@ def test_nothing_changes_in_the_other_calls_without_a_stream(name, world, monkey
     del world.made[:]
     out = _tensors(call(None))
     assert all(t.under == "the caller's" and t.kept_for == [] for t in out) and len(world.launches) == 1
+
+
+@pytest.mark.parametrize("device,current,makes,switched", [(0, 5, False, False), (0, 7, False, False), (0, 5, True, False),
+                                                           (0, 7, True, True), (1, 5, False, True), (1, 5, True, True),
+                                                           (1, 7, True, True)])
+def test_the_stream_is_made_current_only_where_that_matters(device, current, makes, switched, world, monkeypatch):
+    """A call that allocates, on a stream that is not the current one, or any call on another device's."""
+    monkeypatch.setattr(fq, "_has_device", True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: device)
+    monkeypatch.setattr(fq, "_current_stream", lambda: current)
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
+    q = mx(40, 32)
+    out = fq.fq_mx_quantize(given(40, 32), out=None if makes else q, sides=fq.FQ_MX_BOTH, stream=stream)
+    fq.fq_gemm(fq.FQ_OP_NT, fq.QTensor(40, 32), fq.QTensor(48, 32), out=None if makes else given(40, 48), stream=stream)
+    assert [s for _, s in world.launches] == [stream if switched else "the caller's"] * 2
+    assert out.storage.kept_for == (["the caller's"] if makes and switched else [])
