@@ -267,7 +267,7 @@ _has_device = None
 
 def _under(stream, allocates):
     global _has_device
-    if stream is None:
+    if not hasattr(stream, "stream_id"):        # None, or an object with a handle alone, which torch cannot make current
         return _no_context
     torch = _t()
     if _has_device is None:

@@ -75,6 +75,7 @@ def world(monkeypatch):
         return w.made[-1]
 
     fq.MxTensor(1, 1, device="cpu")                     # the native module is looked for with the library itself
+    monkeypatch.setattr(fq, "_has_device", False)
     monkeypatch.setattr(torch.cuda, "stream", under)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: w.current)
     monkeypatch.setattr(torch, "empty", empty)
@@ -108,7 +109,7 @@ def returned(r):
 
 @pytest.mark.parametrize("name", MX_CALLS)
 def test_memory_of_an_mx_call_is_allocated_under_its_stream(name, world):
-    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0, stream_id=3)
     q, w = mx(40, 32), mx(48, 32)
     del world.made[:]
     r = returned(MX_CALLS[name](stream, q, w))
@@ -132,7 +133,7 @@ def test_nothing_changes_without_a_stream(name, world, monkeypatch):
 
 
 def test_what_the_caller_gives_stays_the_callers(world):
-    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0, stream_id=3)
     q, w, y = mx(40, 32), mx(48, 32), given(40, 48)
     del world.made[:]
     fq.fq_mx_quantize(given(40, 32), out=q, stream=stream)
@@ -179,7 +180,7 @@ INT8_CALLS = ["quantize", "quantize_sr", "quantize_topk", "gemm", "gemm_plain", 
 
 @pytest.mark.parametrize("name", INT8_CALLS)
 def test_memory_of_the_other_calls_is_allocated_under_their_stream(name, world):
-    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0, stream_id=3)
     call = _int8_calls()[name]
     del world.made[:]
     out = _tensors(call(stream))
@@ -209,9 +210,16 @@ def test_the_stream_is_made_current_only_where_that_matters(device, current, mak
     monkeypatch.setattr(fq, "_has_device", True)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: device)
     monkeypatch.setattr(fq, "_current_stream", lambda: current)
-    stream = types.SimpleNamespace(cuda_stream=5, device_index=0)
+    stream = types.SimpleNamespace(cuda_stream=5, device_index=0, stream_id=3)
     q = mx(40, 32)
     out = fq.fq_mx_quantize(given(40, 32), out=None if makes else q, sides=fq.FQ_MX_BOTH, stream=stream)
     fq.fq_gemm(fq.FQ_OP_NT, fq.QTensor(40, 32), fq.QTensor(48, 32), out=None if makes else given(40, 48), stream=stream)
     assert [s for _, s in world.launches] == [stream if switched else "the caller's"] * 2
     assert out.storage.kept_for == (["the caller's"] if makes and switched else [])
+
+
+def test_an_object_with_a_handle_alone_is_launched_on(world):
+    handle = types.SimpleNamespace(cuda_stream=5)
+    q = fq.fq_quantize(given(40, 32), fq.FQ_CRIT_NONE, 0.0, stream=handle)
+    fq.fq_gemm(fq.FQ_OP_NT, q, q, stream=handle)
+    assert [s for _, s in world.launches] == ["the caller's"] * 2 and q.storage.kept_for == []
