@@ -525,10 +525,11 @@ hipError_t split(const MxGemmParams& p, hipStream_t st) {
 int64_t tiles_of(int64_t M, int64_t N, int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); }
 
 // Microseconds that the tiles of 256 x 256 (one workgroup per compute unit), of 128 x 256 (one) and of 128 x 128 (two)
-// take, fitted to measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 256 to 11008 on 256 compute units; the
-// model is within 15 % of them where the two are close.  Other numbers of units take the same constants, unmeasured.  A full round of 256 x 256 tiles takes 5 + 0.82 per block of the
-// contraction (power holds the clock down), a part of a round less; of 128 x 128 tiles, a quarter of that output a
-// tile, 2.3 + 0.52 per block, half a round or less 1 + 0.11 to 0.29; of 128 x 256 tiles, one to a compute unit, 2.7 + 0.46.
+// take, fitted to measurements of outputs from 1024 x 2048 to 8192 x 8192 and contractions from 256 to 11008 on 256
+// compute units; the model is within 15 % of them where the two are close.  Other numbers of units take the same
+// constants, unmeasured.  A full round of 256 x 256 tiles takes 5 + 0.82 per block of the contraction (power holds the
+// clock down), a part of a round less; of 128 x 128 tiles, a quarter of that output a tile, 2.3 + 0.52 per block, half
+// a round or less 1 + 0.11 to 0.29; of 128 x 256 tiles, one to a compute unit, 2.7 + 0.46.
 // Measured, 128 x 128, 128 x 256 and 256 x 256: 2048 x 4096 over 4096 22.5, 21.7 and 27.7 us, over 11008 51.1, 47.1 and 59.0,
 // 2048 x 11008 over 4096 58.9, 53.2 and 55.3, 512 x 11008 19.4, 18.4 and 25.4, 4096 x 4096 38.9, 38.1 and 34.7,
 // 1024 x 4096 12.8, 16.8 and 24.1, 1100 x 8192 over 2048 17.8, 20.3 and 18.1.
